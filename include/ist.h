@@ -354,8 +354,127 @@ ist_status ist_static_partition_status(void* cuda_stream);
 int64_t ist_kernel_launches(const ist_ctx* ctx);
 
 /* Message for the most recent failing call on this context ("" if none).  ctx may be NULL,
- * in which case the message of the last failing ist_create on this thread is returned. */
+ * in which case the message of the last failing ist_create, or of the last failing call of those
+ * below that take no context, on this thread is returned. */
 const char* ist_last_error(const ist_ctx* ctx);
+
+/*
+ * Operators for the part of a network that stands in front of the partitioned layers (Sec. 2.2,
+ * "IST for other architectures": a trunk that every site holds whole).  The paper has no counterpart;
+ * ist_local_steps_dx gives such a trunk its gradient, these calls normalise what it hands to the head
+ * and update its parameters.  They take no context.  Work is enqueued on cuda_stream (a cudaStream_t,
+ * NULL = legacy default stream) of the current device, asynchronously, and may be captured into a
+ * graph; nothing is allocated and nothing is kept from one call for the next.  Two calls, and two graphs, that may
+ * run at the same time need workspaces of their own.  Invalid arguments return an error and enqueue
+ * nothing; ist_last_error(NULL) has the message.
+ */
+
+/* Element types. */
+enum { IST_T_F32 = 0, IST_T_BF16 = 1 };
+
+/*
+ * Layer normalisation of rows.  x_dev: `rows` rows of `cols` elements, x_stride elements from one row to the
+ * next (>= cols); so are y, dy and dx with theirs.  The rows belong in order to `groups` sites, rows / groups
+ * each (rows must be a multiple of groups), and every site has its own weight and bias
+ * (weight_dev, bias_dev: [groups][cols] fp32; NULL stands for ones and for zeros).  Per row
+ *   mean = sum_j x_j / cols,   rstd = 1 / sqrt(sum_j (x_j - mean)^2 / cols + eps),
+ *   y_j = (x_j - mean) * rstd * weight_j + bias_j.
+ * mean_out_dev, rstd_out_dev: [rows] fp32 for the backward pass, either may be NULL.  Statistics are taken
+ * in fp32 or wider from the elements' values; y is rounded once, to nearest even.  A row that holds an infinity or
+ * a NaN comes out as NaN, other rows are not touched by it.  rows = 0 is allowed.  0 < eps < inf.
+ * 1 <= cols <= 2^30, 0 <= rows < 2^31, 1 <= groups < 2^31.  Outputs must not overlap inputs or one another
+ * (rows of one buffer that interleave without sharing elements are fine).  Elements between the rows are left as they are.
+ */
+ist_status ist_layer_norm_forward(const void* x_dev, int x_type, int64_t x_stride, int64_t rows, int64_t cols,
+                                  int groups, const float* weight_dev, const float* bias_dev, float eps, void* y_dev,
+                                  int y_type, int64_t y_stride, float* mean_out_dev, float* rstd_out_dev,
+                                  void* cuda_stream);
+
+/*
+ * The way back, from what the forward pass read and returned: with h = (x - mean) * rstd and g = dy * weight,
+ *   dx_j = rstd * (g_j - sum_i g_i / cols - h_j * sum_i g_i h_i / cols)   (x's type),
+ *   dweight = sum over the site's rows of dy * h,   dbias = sum over the site's rows of dy   ([groups][cols] fp32).
+ * dx_out_dev, dweight_out_dev and dbias_out_dev may be NULL where they are not wanted (not all three).  The sums over rows
+ * are added in an order that depends on the shape alone, so results are the same from call to call.  rows = 0 gives
+ * zeros for dweight and dbias.  workspace_dev: at least ist_layer_norm_workspace_bytes(rows, cols, groups) bytes
+ * (0 on invalid arguments), 16-byte aligned, not needed (may be NULL) if neither dweight nor dbias is wanted; its content means nothing before and
+ * after the call.
+ */
+size_t ist_layer_norm_workspace_bytes(int64_t rows, int64_t cols, int groups);
+ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, int64_t dy_stride, const void* x_dev, int x_type,
+                                   int64_t x_stride, int64_t rows, int64_t cols, int groups, const float* weight_dev,
+                                   const float* mean_dev, const float* rstd_dev, void* dx_out_dev, int64_t dx_stride,
+                                   float* dweight_out_dev, float* dbias_out_dev, void* workspace_dev,
+                                   size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * One AdamW step over many tensors.  For every parameter, with gradient g, step number t (1 for the first) and
+ * clipping factor c:
+ *   g' = c g,   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2,
+ *   p = p - lr weight_decay p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),
+ * and, where param_bf16 is given, param_bf16 = p rounded to bf16 (to nearest even).
+ * c = max_norm / norm if max_norm > 0 and norm > max_norm, else 1; norm is the square root of the sum of g^2 over all
+ * tensors of the call.  A norm that is not finite is no error: the factor follows from the same rule (0 for an infinite norm,
+ * 1 for a NaN), and what is not finite in the gradients reaches the parameters and states that it belongs to.
+ *
+ * States (state_bits): 32: exp_avg, exp_avg_sq are fp32 [n] (m and v).  8: they are one byte per value,
+ * and the blocks of IST_ADAMW_BLOCK consecutive values of a tensor share one int16 each in exp_avg_base and
+ * exp_avg_sq_base ([ceil(n / IST_ADAMW_BLOCK)]): a code c > 0 of 8 bits (v), or of the lower 7 bits (m, whose bit 7 is the
+ * sign), is the fp32 number with the bit pattern (base + c) << 20, code 0 is zero, and the largest code (255, 127) stands for a value
+ * that is not finite (infinity for v, NaN for m).  So values have 3 bits behind the leading one, and a block reaches 2^31 (v)
+ * or 2^15 (m) below its largest value, from which the base is taken anew in every step.  Zeros everywhere are the states
+ * before the first step.  The parameter is updated from m and v before they are rounded.  Rounding is random and keeps the mean (to
+ * nearest, an average that moves by a thousandth per step would stand still): a value's fp32 bit pattern plus 20 random
+ * bits is cut at bit 20; the random bits are 16 r + 8, with r for elements 2 i and 2 i + 1 of tensor j from word w = the (i+1)-th output
+ * of a SplitMix64 generator seeded with the (j+1)-th output of one seeded with the t-th output of one seeded with `seed`:
+ * bits 0..15 (m) and 16..31 (v) of w for element 2 i, 32..47 and 48..63 for element 2 i + 1.  What falls below the block's
+ * range becomes zero (m) or the smallest code (v: a divisor must not vanish).
+ *
+ * A tensor with n = 0 or grad = NULL is passed over (its number j still counts).  The tensors' arrays must not overlap one
+ * another, but for gradients, which are only read.  Arrays need the alignment of their elements; arrays that start on 16 bytes (on 4
+ * bytes those of 1-byte codes) are faster.  The table of tensors and the arguments are read during the call.
+ * step, lr: of this step.  A graph replays the arguments of its capture, so for a captured step they may come from
+ * the device instead: step_dev (int64), lr_dev (fp32), not NULL, are read when the kernels run, in place of step and lr.
+ * norm_out_dev (may be NULL): receives the norm (fp32) if max_norm > 0.
+ * workspace_dev: with max_norm > 0 at least ist_adamw_workspace_bytes(count) bytes, 16-byte aligned; else not
+ * needed.  Its content means nothing before and after the call.
+ * Needs 0 <= beta < 1 for both, eps > 0, step >= 1, finite lr and weight decays, max_norm >= 0 (infinity: no clipping, but the norm is taken), at most 2^40 values.
+ */
+#define IST_ADAMW_BLOCK 128
+typedef struct ist_adamw_tensor {
+  float* param;
+  const void* grad;
+  void* exp_avg;
+  void* exp_avg_sq;
+  int16_t* exp_avg_base;    /* 8 bits only */
+  int16_t* exp_avg_sq_base; /* 8 bits only */
+  void* param_bf16;         /* may be NULL */
+  int64_t n;
+  double weight_decay;
+} ist_adamw_tensor;
+typedef struct ist_adamw_args {
+  double lr, beta1, beta2, eps;
+  double max_norm; /* 0: no clipping */
+  int64_t step;
+  uint64_t seed; /* 8 bits only */
+  int32_t state_bits;
+  int32_t grad_type;
+  const int64_t* step_dev; /* may be NULL */
+  const float* lr_dev;     /* may be NULL */
+  float* norm_out_dev;     /* may be NULL */
+} ist_adamw_args;
+size_t ist_adamw_workspace_bytes(int64_t count);
+ist_status ist_adamw_step(const ist_adamw_tensor* tensors_host, int64_t count, const ist_adamw_args* args,
+                          void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * The values that 8-bit states stand for (to look at, or to keep elsewhere): n codes and ceil(n / IST_ADAMW_BLOCK) bases
+ * each of first and second moments, as above, become n fp32 or bf16 values (out_type; exact in both).  Either pair of
+ * outputs and its inputs may be NULL.
+ */
+ist_status ist_adamw_state_values(const uint8_t* exp_avg, const int16_t* exp_avg_base, const uint8_t* exp_avg_sq,
+                                  const int16_t* exp_avg_sq_base, int64_t n, int out_type, void* exp_avg_out_dev,
+                                  void* exp_avg_sq_out_dev, void* cuda_stream);
 
 /* Frees the host object.  Does not touch device memory; pending work keeps running. */
 void ist_destroy(ist_ctx* ctx);

@@ -9,6 +9,7 @@ import ctypes
 import os
 from typing import List, Optional, Sequence, Tuple
 
+import numpy as np
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -27,9 +28,13 @@ EXPORTS = [
     "ist_partition_layer_static", "ist_norm_workspace_bytes", "ist_enable_normalization", "ist_calibrate",
     "ist_set_subnet_range", "ist_packed_layer", "ist_workspace_bytes2", "ist_create2",
     "ist_selftest_wait_expiry", "ist_subnet_slice_shape", "ist_static_partition_status", "ist_local_steps_dx",
+    "ist_layer_norm_forward", "ist_layer_norm_workspace_bytes", "ist_layer_norm_backward", "ist_adamw_workspace_bytes",
+    "ist_adamw_step", "ist_adamw_state_values",
 ]
 IST_PART_BALANCED, IST_PART_IID = 0, 1
 IST_STATIC_MAX_NEURONS, IST_STATIC_MAX_SUBNETS = 65536, 64
+IST_T_F32, IST_T_BF16 = 0, 1
+IST_ADAMW_BLOCK = 128
 
 KERNEL_CLASSES = ["partition", "gather", "stage", "fwd", "loss", "dx", "dw_sgd", "bias_sgd", "spmm",
                   "scatter", "eval", "norm"]
@@ -45,6 +50,29 @@ class IstInput(ctypes.Structure):
         ("val", ctypes.c_void_p),
         ("stride_subnet", ctypes.c_int64),
         ("stride_step", ctypes.c_int64),
+    ]
+
+
+# One row of ist_adamw_step's table.
+ADAMW_TENSOR = np.dtype([(name, np.uint64) for name in ("param", "grad", "exp_avg", "exp_avg_sq", "exp_avg_base",
+                                                         "exp_avg_sq_base", "param_bf16")]
+                        + [("n", np.int64), ("weight_decay", np.float64)])
+
+
+class AdamWArgs(ctypes.Structure):
+    _fields_ = [
+        ("lr", ctypes.c_double),
+        ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double),
+        ("eps", ctypes.c_double),
+        ("max_norm", ctypes.c_double),
+        ("step", ctypes.c_int64),
+        ("seed", ctypes.c_uint64),
+        ("state_bits", ctypes.c_int32),
+        ("grad_type", ctypes.c_int32),
+        ("step_dev", ctypes.c_void_p),
+        ("lr_dev", ctypes.c_void_p),
+        ("norm_out_dev", ctypes.c_void_p),
     ]
 
 
@@ -117,6 +145,19 @@ def _load() -> ctypes.CDLL:
                                      ctypes.POINTER(sz)]
     lib.ist_packed_layer.restype = i32
     lib.ist_destroy.argtypes = [vp]
+    f32 = ctypes.c_float
+    lib.ist_layer_norm_forward.argtypes = [vp, i32, i64, i64, i64, i32, vp, vp, f32, vp, i32, i64, vp, vp, vp]
+    lib.ist_layer_norm_forward.restype = ctypes.c_int32
+    lib.ist_layer_norm_workspace_bytes.argtypes = [i64, i64, i32]
+    lib.ist_layer_norm_workspace_bytes.restype = sz
+    lib.ist_layer_norm_backward.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, i32, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+    lib.ist_layer_norm_backward.restype = ctypes.c_int32
+    lib.ist_adamw_workspace_bytes.argtypes = [i64]
+    lib.ist_adamw_workspace_bytes.restype = sz
+    lib.ist_adamw_step.argtypes = [vp, i64, ctypes.POINTER(AdamWArgs), vp, sz, vp]
+    lib.ist_adamw_step.restype = ctypes.c_int32
+    lib.ist_adamw_state_values.argtypes = [vp, vp, vp, vp, i64, i32, vp, vp, vp]
+    lib.ist_adamw_state_values.restype = ctypes.c_int32
     return lib
 
 
@@ -372,3 +413,252 @@ class Ist:
         loss = self.local_steps(X, y, lr, K, batch, loss_out=loss_out, want_loss=want_loss)
         self.reassemble()
         return loss
+
+
+# --- operators for a trunk in front of the partitioned layers: no context -------------------------------
+
+_TYPES = {torch.float32: IST_T_F32, torch.bfloat16: IST_T_BF16}
+
+
+def _refuse(message: str):
+    raise IstError(IST_ERR_ARG, message)
+
+
+def _call(device: torch.device, stream: Optional[torch.cuda.Stream], function, *args):
+    """function(*args, stream) with `device` current, on `stream` or the device's current stream."""
+    index = device.index
+    if stream is not None and stream.device_index != index:
+        _refuse(f"the stream belongs to another device than {device}")
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _call(device, stream, function, *args)
+    status = function(*args, (stream if stream is not None else torch.cuda.current_stream(index)).cuda_stream)
+    if status != IST_OK:
+        raise IstError(status, lib.ist_last_error(None).decode())
+
+
+def _rows(t: torch.Tensor, name: str, cols: int, device: torch.device, rows: Optional[int] = None) -> Tuple[int, int, int]:
+    """(element type, rows, stride) of a tensor whose last dimension is `cols` elements that lie together."""
+    if t.device != device or device.type != "cuda":
+        _refuse(f"{name} is on {t.device}: one CUDA device for all tensors is needed")
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise TypeError(f"unsupported dtype {t.dtype} of {name}")
+    if t.dim() == 0 or t.shape[-1] != cols or (cols > 1 and t.stride(-1) != 1):
+        _refuse(f"{name}'s last dimension must be {cols} adjacent elements")
+    n = t.numel() // cols
+    if rows is not None and n != rows:
+        _refuse(f"{name} has {n} rows, not {rows}")
+    if n <= 1 or t.is_contiguous():
+        return kind, n, cols
+    if t.dim() != 2:
+        try:
+            t = t.view(-1, cols)
+        except RuntimeError:
+            _refuse(f"{name}'s leading dimensions have no common stride")
+    return kind, n, t.stride(0)
+
+
+def _vector(t: Optional[torch.Tensor], name: str, count: int, device: torch.device) -> Optional[int]:
+    if t is None:
+        return None
+    if t.device != device or t.dtype != torch.float32 or t.numel() != count or not t.is_contiguous():
+        _refuse(f"{name} must be {count} contiguous fp32 values on {device}")
+    return t.data_ptr()
+
+
+def _norm_shape(x: torch.Tensor, groups: int) -> Tuple[int, torch.device]:
+    if x.dim() == 0 or x.shape[-1] == 0:
+        _refuse("x needs a last dimension of at least one element")
+    if not 1 <= groups < 2 ** 31:
+        _refuse("groups must be in 1..2^31 - 1")
+    return x.shape[-1], x.device
+
+
+def ist_layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                           eps: float = 1e-5, groups: int = 1, y: Optional[torch.Tensor] = None,
+                           y_dtype: Optional[torch.dtype] = None, want_stats: bool = True,
+                           stream: Optional[torch.cuda.Stream] = None):
+    """Layer norm over x's last dimension (fp32 or bf16; rows may have a stride).  weight, bias: fp32 [groups][cols], the
+    rows belong in order to `groups` sites.  Returns (y, mean, rstd), y of y_dtype (default x's) or written into the tensor
+    `y`; mean and rstd are fp32 [rows], or None without want_stats."""
+    cols, dev = _norm_shape(x, groups)
+    x_type, rows, x_stride = _rows(x, "x", cols, dev)
+    if y is None:
+        with torch.cuda.stream(stream):      # what a call allocates belongs to the stream it runs on
+            y = torch.empty(x.shape, dtype=y_dtype if y_dtype is not None else x.dtype, device=dev)
+    elif y_dtype is not None and y.dtype != y_dtype:
+        _refuse(f"y is {y.dtype}, not {y_dtype}")
+    y_type, _, y_stride = _rows(y, "y", cols, dev, rows)
+    mean = rstd = None
+    if want_stats:
+        with torch.cuda.stream(stream):
+            mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
+    _call(dev, stream, lib.ist_layer_norm_forward, x.data_ptr(), x_type, x_stride, rows, cols, groups,
+          _vector(weight, "weight", groups * cols, dev), _vector(bias, "bias", groups * cols, dev), eps, y.data_ptr(), y_type,
+          y_stride, _ptr(mean), _ptr(rstd))
+    return y, mean, rstd
+
+
+def ist_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor,
+                            rstd: torch.Tensor, groups: int = 1, want_dx: bool = True, want_dweight: bool = True,
+                            want_dbias: bool = True, dx: Optional[torch.Tensor] = None,
+                            stream: Optional[torch.cuda.Stream] = None):
+    """(dx, dweight, dbias) from the gradient of ist_layer_norm_forward's output and what that call read and returned; dx
+    has x's type (or is written into the tensor `dx`), the others are fp32 [groups][cols], None where not wanted."""
+    cols, dev = _norm_shape(x, groups)
+    x_type, rows, x_stride = _rows(x, "x", cols, dev)
+    dy_type, _, dy_stride = _rows(dy, "dy", cols, dev, rows)
+    dx_stride = 0
+    if dx is not None:
+        if dx.dtype != x.dtype:
+            _refuse("dx must have x's dtype")
+    elif want_dx:
+        with torch.cuda.stream(stream):
+            dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    if dx is not None:
+        _, _, dx_stride = _rows(dx, "dx", cols, dev, rows)
+    dweight = dbias = workspace = None
+    nbytes = 0
+    with torch.cuda.stream(stream):
+        if want_dweight:
+            dweight = torch.empty((groups, cols), dtype=torch.float32, device=dev)
+        if want_dbias:
+            dbias = torch.empty((groups, cols), dtype=torch.float32, device=dev)
+        if want_dweight or want_dbias:
+            nbytes = lib.ist_layer_norm_workspace_bytes(rows, cols, groups)
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _call(dev, stream, lib.ist_layer_norm_backward, dy.data_ptr(), dy_type, dy_stride, x.data_ptr(), x_type, x_stride, rows, cols,
+          groups, _vector(weight, "weight", groups * cols, dev), _vector(mean, "mean", rows, dev),
+          _vector(rstd, "rstd", rows, dev), _ptr(dx), dx_stride, _ptr(dweight), _ptr(dbias), _ptr(workspace), nbytes)
+    return dx, dweight, dbias
+
+
+class AdamW:
+    """AdamW over a list of fp32 tensors, one ist_adamw_step per step(): borrows the parameters (and their bf16 operand
+    `copies`, where given) and owns the states, unless they are handed in.
+
+    state: {"exp_avg", "exp_avg_sq"} and with state_bits = 8 {"exp_avg_base", "exp_avg_sq_base"}: flat tensors in which
+    tensor i starts at offsets[i], a multiple of IST_ADAMW_BLOCK values; zeros before the first step.
+    weight_decay: a number, or one per tensor.  max_norm: bound of the global gradient norm (None: no clipping).
+    step: steps taken so far.  step_dev (int64 [1]), lr_dev (fp32 [1]): device scalars that replace the host's step and lr,
+    for steps that are captured into a graph; step() then adds one to step_dev on the stream before the update.
+    A step runs on `stream` or on the device's current stream."""
+
+    def __init__(self, params: Sequence[torch.Tensor], lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999),
+                 eps: float = 1e-8, weight_decay=0.01, state_bits: int = 32, max_norm: Optional[float] = None,
+                 copies: Optional[Sequence[torch.Tensor]] = None, state: Optional[dict] = None, seed: int = 0, step: int = 0,
+                 step_dev: Optional[torch.Tensor] = None, lr_dev: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None):
+        self.params, self.copies = list(params), None if copies is None else list(copies)
+        if not self.params:
+            _refuse("no parameters")
+        self.device = dev = self.params[0].device
+        if dev.type != "cuda":
+            _refuse(f"parameters are on {dev}: a CUDA device is needed")
+        if state_bits not in (8, 32):
+            _refuse("state_bits is 32 or 8")
+        self.lr, self.steps, self.stream = float(lr), int(step), stream
+        self.sizes = [p.numel() for p in self.params]
+        room = [-(-n // IST_ADAMW_BLOCK) * IST_ADAMW_BLOCK for n in self.sizes]
+        self.offsets = [0]
+        for r in room:
+            self.offsets.append(self.offsets[-1] + r)
+        total = self.offsets.pop()
+        names = ["exp_avg", "exp_avg_sq"] + (["exp_avg_base", "exp_avg_sq_base"] if state_bits == 8 else [])
+        shapes = {n: (torch.int16, total // IST_ADAMW_BLOCK) if n.endswith("base") else
+                  (torch.uint8 if state_bits == 8 else torch.float32, total) for n in names}
+        if state is None:
+            state = {n: torch.zeros(size, dtype=dtype, device=dev) for n, (dtype, size) in shapes.items()}
+        if set(state) != set(names):
+            _refuse(f"state needs {names}")
+        for n, (dtype, size) in shapes.items():
+            t = state[n]
+            if t.device != dev or t.dtype != dtype or tuple(t.shape) != (size,) or not t.is_contiguous():
+                _refuse(f"state {n} must be {size} contiguous values of {dtype} on {dev}")
+        self.state = dict(state)
+        if self.copies is not None and len(self.copies) != len(self.params):
+            _refuse("one copy per parameter is needed")
+        for name, tensors, dtype in (("parameter", self.params, torch.float32), ("copy", self.copies or [], torch.bfloat16)):
+            for i, t in enumerate(tensors):
+                if t.device != dev or t.dtype != dtype or t.numel() != self.sizes[i] or not t.is_contiguous():
+                    _refuse(f"{name} {i} must be {self.sizes[i]} contiguous values of {dtype} on {dev}")
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+                       for t in self.params + (self.copies or []) + list(self.state.values()) if t.numel())
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            _refuse("parameters, copies and states must not overlap")
+        decay = [float(weight_decay)] * len(self.params) if isinstance(weight_decay, (int, float)) else [float(d) for d in weight_decay]
+        if len(decay) != len(self.params):
+            _refuse("one weight decay per parameter is needed")
+        self.table = np.zeros(len(self.params), ADAMW_TENSOR)
+        self.table["param"] = [p.data_ptr() for p in self.params]
+        for n in names:
+            base, size, per = self.state[n].data_ptr(), self.state[n].element_size(), IST_ADAMW_BLOCK if n.endswith("base") else 1
+            self.table[n] = [base + o // per * size for o in self.offsets]
+        if self.copies is not None:
+            self.table["param_bf16"] = [c.data_ptr() for c in self.copies]
+        self.table["n"], self.table["weight_decay"] = self.sizes, decay
+        for name, t, dtype in (("step_dev", step_dev, torch.int64), ("lr_dev", lr_dev, torch.float32)):
+            if t is not None and (t.device != dev or t.dtype != dtype or t.numel() != 1):
+                _refuse(f"{name} must be one value of {dtype} on {dev}")
+        self.step_dev, self.lr_dev = step_dev, lr_dev
+        self.args = AdamWArgs(lr=self.lr, beta1=betas[0], beta2=betas[1], eps=eps, max_norm=max_norm or 0.0,
+                              seed=seed & (2 ** 64 - 1), state_bits=state_bits, step_dev=_ptr(step_dev), lr_dev=_ptr(lr_dev))
+        self.workspace = None
+        self.workspace_bytes = int(lib.ist_adamw_workspace_bytes(len(self.params))) if max_norm else 0
+        if max_norm:
+            self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
+
+    def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, lr: Optional[float] = None) -> Optional[torch.Tensor]:
+        """One step with `grads` (default: the parameters' .grad), all fp32 or all bf16; a None passes its tensor over.
+        Returns the gradients' norm (fp32 [1]) if they are clipped.  The gradients may be freed or written once the
+        work on the stream that follows allows it, as with any asynchronous call."""
+        if grads is None:
+            grads = [p.grad for p in self.params]
+        if len(grads) != len(self.params):
+            _refuse("one gradient (or None) per parameter is needed")
+        dev, dtype, at = self.device, None, []
+        for i, (g, n) in enumerate(zip(grads, self.sizes)):
+            if g is None:
+                at.append(0)
+                continue
+            dtype = dtype or g.dtype
+            if g.dtype != dtype or g.numel() != n or g.device != dev or not g.is_contiguous():
+                _refuse(f"gradient {i} must be {n} contiguous values of {dtype} on {dev}")
+            at.append(g.data_ptr())
+        kind = _TYPES.get(dtype, IST_T_F32 if dtype is None else None)
+        if kind is None:
+            raise TypeError(f"unsupported gradient dtype {dtype}")
+        self.table["grad"] = at
+        args = self.args
+        args.grad_type = kind
+        if lr is not None:
+            self.lr = float(lr)
+        args.lr, args.step = self.lr, self.steps + 1
+        norm = None
+        if self.workspace is not None:
+            with torch.cuda.stream(self.stream):
+                norm = torch.empty(1, dtype=torch.float32, device=dev)
+            args.norm_out_dev = norm.data_ptr()
+        if self.step_dev is not None:
+            with torch.cuda.stream(self.stream):        # None: the current stream stays
+                self.step_dev.add_(1)
+        _call(dev, self.stream, lib.ist_adamw_step, self.table.ctypes.data, len(self.params), args, _ptr(self.workspace),
+              self.workspace_bytes)
+        self.steps += 1
+        return norm
+
+    def state_values(self, dtype: torch.dtype = torch.float32) -> Tuple[torch.Tensor, torch.Tensor]:
+        """First and second moments as flat tensors of `dtype` (fp32 or bf16), tensor i from offsets[i] on."""
+        if dtype not in _TYPES:
+            raise TypeError(f"unsupported dtype {dtype}")
+        m, v = self.state["exp_avg"], self.state["exp_avg_sq"]
+        if "exp_avg_base" not in self.state:
+            with torch.cuda.stream(self.stream):
+                return m.to(dtype, copy=True), v.to(dtype, copy=True)
+        with torch.cuda.stream(self.stream):
+            out = torch.empty((2, m.numel()), dtype=dtype, device=self.device)
+        a, b = out.unbind(0)
+        _call(self.device, self.stream, lib.ist_adamw_state_values, m.data_ptr(), self.state["exp_avg_base"].data_ptr(),
+              v.data_ptr(), self.state["exp_avg_sq_base"].data_ptr(), m.numel(), _TYPES[dtype], a.data_ptr(), b.data_ptr())
+        return a, b

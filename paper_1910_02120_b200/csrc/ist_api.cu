@@ -842,6 +842,16 @@ extern "C" size_t ist_workspace_bytes2(const int64_t* layer_dims, int n_dims, in
   return tmp.plan.total;
 }
 
+int ist::fail_call(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  g_create_error = buf;
+  return code;
+}
+
 extern "C" size_t ist_workspace_bytes(const int64_t* layer_dims, int n_dims, int S, int precision,
                                       int max_batch, int input_is_csr) {
   return ist_workspace_bytes2(layer_dims, n_dims, S, precision, max_batch, input_is_csr, IST_PART_BALANCED);

@@ -11,6 +11,13 @@ struct Launch {
   void count(int n = 1) const { if (counter) *counter += n; }
 };
 
+// ---- ist_api.cu ---------------------------------------------------------------------------
+// Keeps the message of a call without a context (ist_last_error(NULL)) and returns `code` (an ist_status).
+int fail_call(int code, const char* fmt, ...);
+
+// ---- gemm_tc.cu ---------------------------------------------------------------------------
+int sm_count();   // of the device current at the first call
+
 // ---- partition.cu -----------------------------------------------------------------------
 // Balanced random partition of {0..N-1} into S groups from SplitMix64 keys (see ist.h).
 // Outputs: idx [N] (group-major, ascending inside a group), off [S+1].  Scratch arrays live in
