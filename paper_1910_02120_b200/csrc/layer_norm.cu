@@ -4,10 +4,9 @@
 #include <algorithm>
 #include <cmath>
 
-#include "kernels.h"
+#include "norm_rows.cuh"
 
-using namespace ist;
-
+namespace ist {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
@@ -193,12 +192,19 @@ const char* bad_shape(int64_t rows, int64_t cols, int groups) {
   return nullptr;
 }
 
-// Parts that a site's rows are cut into for the sums over them: enough blocks for the GPU, at least a row each.
+// Parts that a site's rows are cut into for the sums over them: enough blocks for the GPU, but 16,384 elements at least
+// to a part.
 int parts_of(int64_t rows, int64_t cols, int groups) {
-  const int64_t chunks = ceil_div(cols, kColumns) * groups;
-  int64_t parts = ceil_div((int64_t)sm_count() * 8, chunks);
-  parts = std::min<int64_t>(parts, ceil_div(rows / groups, 4 * kLanes));
-  return (int)std::max<int64_t>(1, parts);
+  const int64_t site_rows = rows / groups;
+  int64_t parts, least;
+  if (cols <= kNormWidest) {
+    parts = (int64_t)sm_count() * (cols <= 4096 ? 2 : 1) / groups;
+    least = ceil_div(16384, cols);
+  } else {
+    parts = ceil_div((int64_t)sm_count() * 8, ceil_div(cols, kColumns) * groups);
+    least = 4 * kLanes;
+  }
+  return (int)std::max<int64_t>(1, std::min(parts, ceil_div(site_rows, least)));
 }
 
 template <typename F>
@@ -210,6 +216,9 @@ void with_types(int a, int b, F f) {
 }
 
 }  // namespace
+}  // namespace ist
+
+using namespace ist;
 
 extern "C" ist_status ist_layer_norm_forward(const void* x_dev, int x_type, int64_t x_stride, int64_t rows, int64_t cols,
                                              int groups, const float* weight_dev, const float* bias_dev, float eps,
@@ -238,7 +247,9 @@ extern "C" ist_status ist_layer_norm_forward(const void* x_dev, int x_type, int6
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   cudaError_t e = cudaSuccess;
   const unsigned blocks = (unsigned)std::min<int64_t>(rows, (int64_t)sm_count() * 8);
-  with_types(x_type, y_type, [&](auto xt, auto yt) {
+  const NormForward rows_args{x_dev, y_dev, x_stride, y_stride, rows / groups, groups, (int)cols, weight_dev, bias_dev,
+                              mean_out_dev, rstd_out_dev, eps};
+  if (cols > kNormWidest || !norm_forward_rows(rows_args, x_type == IST_T_BF16, y_type == IST_T_BF16, stream, &e)) with_types(x_type, y_type, [&](auto xt, auto yt) {
     using XT = decltype(xt);
     using YT = decltype(yt);
     e = launch_pdl(norm_forward_any_kernel<XT, YT>, dim3(blocks), dim3(kThreads), 0, stream, (const XT*)x_dev, x_stride,
@@ -303,7 +314,16 @@ extern "C" ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, i
   if (chunks * groups * parts >= (int64_t)1 << 31)
     return fail_call(IST_ERR_UNSUPPORTED, "ist_layer_norm_backward: groups * cols is too large");
   float* const part_sums = (float*)workspace_dev;
-  with_types(x_type, dy_type, [&](auto xt, auto dt) {
+  const bool join = sums && parts > 1;
+  const NormBackward rows_args{dy_dev, x_dev, dx_out_dev, dy_stride, x_stride, dx_stride, site_rows, groups, (int)cols, weight_dev,
+                               mean_dev, rstd_dev, join ? part_sums : dweight_out_dev, join ? part_sums + cols : dbias_out_dev,
+                               join ? 2 * cols : cols, parts};
+  bool taken = cols <= kNormWidest && norm_backward_rows(rows_args, x_type == IST_T_BF16, dy_type == IST_T_BF16, stream, &e);
+  if (taken && (e != cudaSuccess || !join)) {
+    if (e != cudaSuccess) return fail_call(IST_ERR_CUDA, "ist_layer_norm_backward: %s", cudaGetErrorString(e));
+    return IST_OK;
+  }
+  if (!taken) with_types(x_type, dy_type, [&](auto xt, auto dt) {
     using XT = decltype(xt);
     using DT = decltype(dt);
     if (dx_out_dev)
