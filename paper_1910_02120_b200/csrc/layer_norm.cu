@@ -127,31 +127,34 @@ __global__ void __launch_bounds__(kColumns* kLanes) norm_columns_any_kernel(cons
   }
 }
 
-// dweight and dbias from the parts' sums.
-__global__ void __launch_bounds__(kColumns* kLanes) norm_join_kernel(const float* parts_sums, int64_t cols, int sites,
-                                                                    int parts, float* dweight, float* dbias) {
-  __shared__ double sh[2][kLanes][kColumns + 1];
+// dweight and dbias from the parts' sums: 32 columns and 32 lanes of parts to a block, so that all of a column's sums are
+// on their way at once.
+constexpr int kJoinLanes = 32;
+__global__ void __launch_bounds__(kColumns* kJoinLanes) norm_join_kernel(const float* parts_sums, int64_t cols, int sites,
+                                                                        int parts, float* dweight, float* dbias) {
+  __shared__ float sh[kJoinLanes][kColumns + 1];
   pdl_wait();
   pdl_trigger();
+  // blocks: [site][dweight, dbias][chunk of columns]
   const int64_t chunks = ceil_div(cols, kColumns);
-  const int64_t j = (int64_t)(blockIdx.x % chunks) * kColumns + threadIdx.x, site = blockIdx.x / chunks;
-  double sw = 0., sb = 0.;
-  if (j < cols)
-    for (int p = threadIdx.y; p < parts; p += kLanes) {
-      const float* in = parts_sums + ((int64_t)p * sites + site) * 2 * cols + j;
-      sw += in[0];
-      sb += in[cols];
-    }
-  sh[0][threadIdx.y][threadIdx.x] = sw;
-  sh[1][threadIdx.y][threadIdx.x] = sb;
-  __syncthreads();
-  if (threadIdx.y < 2 && j < cols) {
-    double s = 0.;
-#pragma unroll
-    for (int u = 0; u < kLanes; ++u) s += sh[threadIdx.y][u][threadIdx.x];
-    float* out = threadIdx.y ? dbias : dweight;
-    if (out) out[site * cols + j] = (float)s;
+  const int64_t j = (int64_t)(blockIdx.x % chunks) * kColumns + threadIdx.x, which = blockIdx.x / chunks % 2;
+  const int64_t site = blockIdx.x / (chunks * 2), step = (int64_t)sites * 2 * cols;
+  float* const out = which ? dbias : dweight;
+  if (!out) return;
+  float s = 0.f;
+  if (j < cols) {
+    const float* in = parts_sums + (site * 2 + which) * cols + j + threadIdx.y * step;
+#pragma unroll 4
+    for (int p = threadIdx.y; p < parts; p += kJoinLanes, in += kJoinLanes * step) s += *in;
   }
+  sh[threadIdx.y][threadIdx.x] = s;
+  __syncthreads();
+  // lane x of warp y: part lane x of column y
+  s = sh[threadIdx.x][threadIdx.y];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  const int64_t c = (int64_t)(blockIdx.x % chunks) * kColumns + threadIdx.y;
+  if (threadIdx.x == 0 && c < cols) out[site * cols + c] = s;
 }
 
 // Rows of an array in memory: `rows` runs of `run` bytes, `pitch` bytes apart.
@@ -198,7 +201,7 @@ int parts_of(int64_t rows, int64_t cols, int groups) {
   const int64_t site_rows = rows / groups;
   int64_t parts, least;
   if (cols <= kNormWidest) {
-    parts = (int64_t)sm_count() * (cols <= 4096 ? 2 : 1) / groups;
+    parts = (int64_t)sm_count() * (cols <= 4096 ? 2 : 1) / norm_cluster(cols) / groups;
     least = ceil_div(16384, cols);
   } else {
     parts = ceil_div((int64_t)sm_count() * 8, ceil_div(cols, kColumns) * groups);
@@ -311,7 +314,7 @@ extern "C" ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, i
   const int64_t site_rows = rows / groups;
   const int64_t chunks = ceil_div(cols, kColumns);
   const int parts = parts_of(rows, cols, groups);
-  if (chunks * groups * parts >= (int64_t)1 << 31)
+  if (chunks * groups * std::max(parts, 2) >= (int64_t)1 << 31)
     return fail_call(IST_ERR_UNSUPPORTED, "ist_layer_norm_backward: groups * cols is too large");
   float* const part_sums = (float*)workspace_dev;
   const bool join = sums && parts > 1;
@@ -336,7 +339,7 @@ extern "C" ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, i
                      rstd_dev, part_sums);
   });
   if (e == cudaSuccess && sums)
-    e = launch_pdl(norm_join_kernel, dim3((unsigned)(chunks * groups)), dim3(kColumns, kLanes), 0, stream,
+    e = launch_pdl(norm_join_kernel, dim3((unsigned)(chunks * groups * 2)), dim3(kColumns, kJoinLanes), 0, stream,
                    (const float*)part_sums, cols, groups, parts, dweight_out_dev, dbias_out_dev);
   if (e != cudaSuccess) return fail_call(IST_ERR_CUDA, "ist_layer_norm_backward: %s", cudaGetErrorString(e));
   return IST_OK;

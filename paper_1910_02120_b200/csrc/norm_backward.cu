@@ -1,5 +1,5 @@
-// Layer norm's way back for rows that fit the threads of a block: dy and x are read once, dx written, and the sums
-// over rows that dweight and dbias need are kept in registers, a column always with the same thread.
+// Layer norm's way back for rows that fit the threads of a block or a cluster: dy and x are read once, dx written, and
+// the sums over rows that dweight and dbias need are kept in registers, a column always with the same thread.
 #include <algorithm>
 #include <mutex>
 
@@ -8,155 +8,165 @@
 namespace ist {
 namespace {
 
-template <typename XT, typename DT, int V, int NV, int TPR, int RB, int D>
+template <typename XT, typename DT, int V, int NV, int TPR, int RB, int D, int CL, bool FULL>
 __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_backward_kernel(const NormBackward a) {
   constexpr int kThreads = TPR > kNormThreads ? TPR : kNormThreads, kSlots = kThreads / TPR, kTile = kSlots * RB;
-  constexpr int C = NV * V;
+  constexpr int C = NV * V, P = C / 2;
   extern __shared__ __align__(16) char ring[];
-  __shared__ float sh[2 * kThreads / 32 * RB * 2];
+  __shared__ float sh[2 * kThreads / 32 * CL * RB * 2];
   const int t = threadIdx.x % TPR, slot = threadIdx.x / TPR;
-  const int cols = a.cols, x_room = row_room(cols, sizeof(XT), V == 1), room = x_room + row_room(cols, sizeof(DT), V == 1);
-  const int64_t site = blockIdx.x % a.sites, part = blockIdx.x / a.sites;
+  // columns of this block: the row's, or the part of them that is this block's in its cluster
+  const int width = FULL ? TPR * C : part_width(a.cols, CL);
+  const int c0 = CL > 1 ? (int)cluster_rank() * width : 0, cols = CL > 1 ? max(min(a.cols - c0, width), 0) : a.cols;
+  const int x_room = row_room(width, sizeof(XT), V == 1), room = x_room + row_room(width, sizeof(DT), V == 1);
+  const int64_t block = blockIdx.x / CL;
+  const int site = (int)(block % a.sites), part = (int)(block / a.sites);
   // this block's rows of its site
-  const int64_t begin = a.site_rows * part / a.parts, end = a.site_rows * (part + 1) / a.parts;
-  const int64_t row0 = site * a.site_rows;
-  const XT* const x = (const XT*)a.x + row0 * a.x_ld;
-  const DT* const dy = (const DT*)a.dy + row0 * a.dy_ld;
-  XT* const dx = a.dx ? (XT*)a.dx + row0 * a.dx_ld : nullptr;
-  const float inv = 1.f / (float)cols;
-  const int tiles = (int)ceil_div(end - begin, kTile);
-  int turn = 0;
+  const int row0 = (int)(site * a.site_rows), begin = row0 + (int)(a.site_rows * part / a.parts);
+  const int end = row0 + (int)(a.site_rows * (part + 1) / a.parts);
+  const XT* const x = (const XT*)a.x + c0;
+  const DT* const dy = (const DT*)a.dy + c0;
+  const float inv = 1.f / (float)a.cols;
+  int r = begin + slot * RB, in_r = r, stage = 0, in_stage = 0, turn = 0;
 
-  auto row_of = [&](int k, int j) { return begin + (int64_t)k * kTile + slot * RB + j; };
-  auto buffer = [&](int k, int j) { return ring + ((k % D * kSlots + slot) * RB + j) * room; };
-  auto fetch = [&](int k) {
-    if (k < tiles) {
+  auto buffer = [&](int stage, int j) { return ring + ((stage * kSlots + slot) * RB + j) * room; };
+  auto fetch = [&]() {
 #pragma unroll
-      for (int j = 0; j < RB; ++j) {
-        const int64_t r = row_of(k, j);
-        if (r < end) {
-          fetch_row<XT, V, TPR>(x + r * a.x_ld, cols, buffer(k, j), t);
-          fetch_row<DT, V, TPR>(dy + r * a.dy_ld, cols, buffer(k, j) + x_room, t);
-        }
+    for (int j = 0; j < RB; ++j)
+      if (in_r + j < end) {
+        fetch_row<XT, V, NV, TPR, FULL>(x + (int64_t)(in_r + j) * a.x_ld, cols, buffer(in_stage, j), t);
+        fetch_row<DT, V, NV, TPR, FULL>(dy + (int64_t)(in_r + j) * a.dy_ld, cols, buffer(in_stage, j) + x_room, t);
       }
-    }
+    in_r += kTile;
+    if (++in_stage == D) in_stage = 0;
     copy_commit();
   };
   // what of the next tile is carried in registers: the rows' statistics, and elements that no copy takes
   float next_mean[RB], next_rstd[RB];
   uint16_t odd_x[RB], odd_d[RB];
-  auto fetch_more = [&](int k) {
+  auto fetch_more = [&](int r) {
 #pragma unroll
     for (int j = 0; j < RB; ++j) {
-      const int64_t r = row_of(k, j);
-      const bool live = r < end;
-      next_mean[j] = live ? a.mean[row0 + r] : 0.f;
-      next_rstd[j] = live ? a.rstd[row0 + r] : 0.f;
+      const bool live = r + j < end;
+      next_mean[j] = live ? a.mean[r + j] : 0.f;
+      next_rstd[j] = live ? a.rstd[r + j] : 0.f;
       if (V == 1) {
-        odd_x[j] = live ? load_odd(x + r * a.x_ld, cols, t) : (uint16_t)0;
-        odd_d[j] = live ? load_odd(dy + r * a.dy_ld, cols, t) : (uint16_t)0;
+        odd_x[j] = live ? load_odd(x + (int64_t)(r + j) * a.x_ld, cols, t) : (uint16_t)0;
+        odd_d[j] = live ? load_odd(dy + (int64_t)(r + j) * a.dy_ld, cols, t) : (uint16_t)0;
       }
     }
   };
+  auto here = [&](int i) { return FULL || (t + i * TPR) * V < cols; };
 
   pdl_wait();
   pdl_trigger();
 #pragma unroll
-  for (int k = 0; k < D - 1; ++k) fetch(k);
-  fetch_more(0);
-  float w[C], aw[C], ab[C];
+  for (int k = 0; k < D - 1; ++k) fetch();
+  fetch_more(r);
+  pair w[P], aw[P], ab[P];
   {
-    const float* const ws = a.weight ? a.weight + site * cols : nullptr;
+    const float* const ws = a.weight ? a.weight + (int64_t)site * a.cols + c0 : nullptr;
     const bool wide = ((uintptr_t)ws & 15) == 0;
+    float f[C];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (t + i * TPR) * V;
 #pragma unroll
-      for (int e = 0; e < V; ++e) w[i * V + e] = 1.f;
-      if (ws && c < cols) load_vector<V>(ws + c, wide, w + i * V);
+      for (int e = 0; e < V; ++e) f[i * V + e] = 1.f;
+      if (ws && here(i)) load_vector<V>(ws + (t + i * TPR) * V, wide, f + i * V);
+    }
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+      w[e] = make_pair2(f[2 * e], f[2 * e + 1]);
+      aw[e] = ab[e] = both(0.f);
     }
   }
-#pragma unroll
-  for (int e = 0; e < C; ++e) aw[e] = ab[e] = 0.f;
-  for (int k = 0; k < tiles; ++k) {
-    fetch(k + D - 1);
+  const int tiles = (int)ceil_div(end - begin, kTile);
+  for (int k = 0; k < tiles; ++k, r += kTile) {
+    fetch();
     copy_wait<D - 1>();
-    float mean[RB], rstd[RB];
+    float rstd[RB];
+    pair minus[RB];
 #pragma unroll
     for (int j = 0; j < RB; ++j) {
-      mean[j] = next_mean[j];
+      minus[j] = both(-next_mean[j]);
       rstd[j] = next_rstd[j];
-      const int64_t r = row_of(k, j);
-      if (V == 1 && r < end) {
-        store_odd(x + r * a.x_ld, cols, buffer(k, j), t, odd_x[j]);
-        store_odd(dy + r * a.dy_ld, cols, buffer(k, j) + x_room, t, odd_d[j]);
+      if (V == 1 && r + j < end) {
+        store_odd(x + (int64_t)(r + j) * a.x_ld, cols, buffer(stage, j), t, odd_x[j]);
+        store_odd(dy + (int64_t)(r + j) * a.dy_ld, cols, buffer(stage, j) + x_room, t, odd_d[j]);
       }
     }
     if (V == 1) row_barrier<TPR>();
-    fetch_more(k + 1);
-    float h[RB][C], g[RB][C], s[2 * RB];
+    fetch_more(r + kTile);
+    pair h[RB][P], g[RB][P];
+    float s[2 * RB];
 #pragma unroll
     for (int j = 0; j < RB; ++j) {
-      const int64_t r = row_of(k, j);
-      const bool live = r < end;
-      const char* const bx = buffer(k, j) + (V == 1 ? (uintptr_t)(x + r * a.x_ld) & 15 : 0);
-      const char* const bd = buffer(k, j) + x_room + (V == 1 ? (uintptr_t)(dy + r * a.dy_ld) & 15 : 0);
-      float s0 = 0.f, s1 = 0.f;
+      const bool live = r + j < end;
+      const char* const bx =
+          buffer(stage, j) + (V == 1 ? (int)((uintptr_t)(x + (int64_t)(r + j) * a.x_ld) & 15) : 0) + t * (V * (int)sizeof(XT));
+      const char* const bd = buffer(stage, j) + x_room +
+                             (V == 1 ? (int)((uintptr_t)(dy + (int64_t)(r + j) * a.dy_ld) & 15) : 0) + t * (V * (int)sizeof(DT));
+      float xv[C], dv[C];
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int c = (t + i * TPR) * V;
-        float xv[V], dv[V];
-        if (live && c < cols) {
-          unpack<XT, V>(bx + c * sizeof(XT), xv);
-          unpack<DT, V>(bd + c * sizeof(DT), dv);
+        if (live && here(i)) {
+          unpack<XT, V>(bx + i * (TPR * V * sizeof(XT)), xv + i * V);
+          unpack<DT, V>(bd + i * (TPR * V * sizeof(DT)), dv + i * V);
         } else {
 #pragma unroll
-          for (int e = 0; e < V; ++e) { xv[e] = mean[j]; dv[e] = 0.f; }
-        }
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const int q = i * V + e;
-          h[j][q] = (xv[e] - mean[j]) * rstd[j];
-          aw[q] = fmaf(dv[e], h[j][q], aw[q]);
-          ab[q] += dv[e];
-          g[j][q] = dv[e] * w[q];
-          s0 += g[j][q];
-          s1 = fmaf(g[j][q], h[j][q], s1);
+          for (int e = 0; e < V; ++e) xv[i * V + e] = dv[i * V + e] = 0.f;     // dy = 0 leaves all sums as they are
         }
       }
-      s[j] = s0;
-      s[RB + j] = s1;
+      pair s0 = both(0.f), s1 = both(0.f);
+      const pair rs = both(rstd[j]);
+#pragma unroll
+      for (int e = 0; e < P; ++e) {
+        const pair d = make_pair2(dv[2 * e], dv[2 * e + 1]);
+        h[j][e] = mul(add(make_pair2(xv[2 * e], xv[2 * e + 1]), minus[j]), rs);
+        g[j][e] = mul(d, w[e]);
+        aw[e] = fma(d, h[j][e], aw[e]);
+        ab[e] = add(ab[e], d);
+        s0 = add(s0, g[j][e]);
+        s1 = fma(g[j][e], h[j][e], s1);
+      }
+      s[j] = first(s0) + second(s0);
+      s[RB + j] = first(s1) + second(s1);
     }
-    if (dx) {
-      row_sums<TPR, 2 * RB>(s, sh, &turn);
+    if (a.dx) {
+      row_sums<TPR, CL, 2 * RB>(s, sh, &turn);
 #pragma unroll
       for (int j = 0; j < RB; ++j) {
-        const int64_t r = row_of(k, j);
-        if (r < end) {
-          const float c0 = s[j] * inv, c1 = s[RB + j] * inv;
+        if (r + j < end) {
+          const pair m0 = both(-s[j] * inv), m1 = both(-s[RB + j] * inv), rs = both(rstd[j]);
+          XT* const to = (XT*)a.dx + c0 + (int64_t)(r + j) * a.dx_ld + t * V;
+          float o[C];
 #pragma unroll
-          for (int i = 0; i < NV; ++i) {
-            const int c = (t + i * TPR) * V;
-            float o[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) o[e] = rstd[j] * fmaf(-h[j][i * V + e], c1, g[j][i * V + e] - c0);
-            if (c < cols) pack<XT, V>(dx + r * a.dx_ld + c, o);
+          for (int e = 0; e < P; ++e) {
+            const pair q = mul(fma(h[j][e], m1, add(g[j][e], m0)), rs);
+            o[2 * e] = first(q);
+            o[2 * e + 1] = second(q);
           }
+#pragma unroll
+          for (int i = 0; i < NV; ++i)
+            if (here(i)) pack<XT, V>(to + i * (TPR * V), o + i * V);
         }
       }
     }
+    if (++stage == D) stage = 0;
     if (V == 1) row_barrier<TPR>();                         // the next fetch writes what this tile was read from
   }
   copy_wait<0>();
+  if (CL > 1) cluster_barrier();                            // no block ends while another may write to its sums
   if (!a.wsum && !a.bsum) return;
+  const int64_t at = ((int64_t)part * a.sites + site) * a.sum_ld + c0;
   // the slots' sums are joined in shared memory, slot after slot
   if (kSlots > 1) {
     __syncthreads();
     float* const f = reinterpret_cast<float*>(ring);        // [slot][2][C][TPR]
 #pragma unroll
     for (int e = 0; e < C; ++e) {
-      f[((slot * 2 + 0) * C + e) * TPR + t] = aw[e];
-      f[((slot * 2 + 1) * C + e) * TPR + t] = ab[e];
+      f[((slot * 2 + 0) * C + e) * TPR + t] = e % 2 ? second(aw[e / 2]) : first(aw[e / 2]);
+      f[((slot * 2 + 1) * C + e) * TPR + t] = e % 2 ? second(ab[e / 2]) : first(ab[e / 2]);
     }
     __syncthreads();
     for (int q = threadIdx.x; q < 2 * C * TPR; q += kThreads) {
@@ -166,68 +176,70 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
       const int which = q / (C * TPR), e = q % (C * TPR) / TPR, tt = q % TPR;
       const int c = (tt + e / V * TPR) * V + e % V;
       float* const out = which ? a.bsum : a.wsum;
-      if (out && c < cols) out[(part * a.sites + site) * a.sum_ld + c] = sum;
+      if (out && c < cols) out[at + c] = sum;
     }
   } else {
-    const int64_t at = (part * a.sites + site) * a.sum_ld;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (t + i * TPR) * V;
+    for (int e = 0; e < C; ++e) {
+      const int c = (t + e / V * TPR) * V + e % V;
       if (c < cols) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          if (a.wsum) a.wsum[at + c + e] = aw[i * V + e];
-          if (a.bsum) a.bsum[at + c + e] = ab[i * V + e];
-        }
+        if (a.wsum) a.wsum[at + c] = e % 2 ? second(aw[e / 2]) : first(aw[e / 2]);
+        if (a.bsum) a.bsum[at + c] = e % 2 ? second(ab[e / 2]) : first(ab[e / 2]);
       }
     }
   }
 }
 
-template <typename XT, typename DT, int V, int NV, int TPR, int RB, int D>
+template <typename XT, typename DT, int V, int NV, int TPR, int RB, int D, int CL, bool FULL>
 cudaError_t launch(const NormBackward& a, cudaStream_t stream) {
   constexpr int kThreads = TPR > kNormThreads ? TPR : kNormThreads, kSlots = kThreads / TPR;
-  const auto kernel = norm_backward_kernel<XT, DT, V, NV, TPR, RB, D>;
+  const auto kernel = norm_backward_kernel<XT, DT, V, NV, TPR, RB, D, CL, FULL>;
+  auto ring = [](int cols) { return D * kSlots * RB * (row_room(cols, sizeof(XT), V == 1) + row_room(cols, sizeof(DT), V == 1)); };
   constexpr int kJoin = kSlots > 1 ? kSlots * 2 * NV * V * TPR * 4 : 0;
-  const int rows = D * kSlots * RB * (row_room(a.cols, sizeof(XT), V == 1) + row_room(a.cols, sizeof(DT), V == 1));
   constexpr int kMost = std::max(kJoin, D * kSlots * RB * (row_room(TPR * V * NV, sizeof(XT), V == 1) + row_room(TPR * V * NV, sizeof(DT), V == 1)));
   static_assert(kMost <= 225 * 1024, "ring too large");
   static std::once_flag once;
   static cudaError_t ready = cudaSuccess;
   std::call_once(once, [&] { ready = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost); });
   if (ready != cudaSuccess) return ready;
-  return launch_pdl(kernel, dim3((unsigned)(a.sites * (int64_t)a.parts)), dim3(kThreads), std::max(rows, kJoin), stream, a);
+  return launch_rows(kernel, (unsigned)((int64_t)a.sites * a.parts * CL), kThreads, std::max(ring(part_width(a.cols, CL)), kJoin), CL, stream, a);
 }
 
 template <typename XT, typename DT>
 bool dispatch(const NormBackward& a, cudaStream_t stream, cudaError_t* e) {
-  constexpr int V = sizeof(XT) == 2 && sizeof(DT) == 2 ? 8 : 4, S = sizeof(XT) + sizeof(DT);
+  constexpr int V = sizeof(XT) == 2 && sizeof(DT) == 2 ? 8 : 4;
   auto fits = [&](const void* p, int64_t ld, int size) { return (((uintptr_t)p | (uintptr_t)(ld * size)) & (V * size - 1)) == 0; };
   const bool pieces = a.cols % V == 0 && fits(a.x, a.x_ld, sizeof(XT)) && fits(a.dy, a.dy_ld, sizeof(DT)) &&
                       (!a.dx || fits(a.dx, a.dx_ld, sizeof(XT)));
   const int n = a.cols;
-#define TAKE(most, v, nv, tpr, rb, d) \
-  if (n <= (most)) return *e = launch<XT, DT, v, nv, tpr, rb, d>(a, stream), true
+#define TAKE(v, nv, tpr, rb, d, cl)                                                                  \
+  if ((v) > 1 && n == (v) * (nv) * (tpr) * (cl))                                                     \
+    return *e = launch<XT, DT, v, nv, tpr, rb, d, cl, (v > 1)>(a, stream), true;                     \
+  if (n <= (v) * (nv) * (tpr) * (cl)) return *e = launch<XT, DT, v, nv, tpr, rb, d, cl, false>(a, stream), true
   if (pieces) {
-    TAKE(64, V, 1, 64 / V, 1, 4);
-    TAKE(128, V, 1, 128 / V, 1, 4);
-    TAKE(256, V, 8 / V, 32, 1, 4);
-    TAKE(512, V, 16 / V, 32, 1, 3);
-    TAKE(1024, V, 16 / V, 64, 1, 3);
-    TAKE(2048, V, 16 / V, 128, 1, 3);
-    TAKE(4096, V, 16 / V, 256, 1, 3);
-    TAKE(8192, V, 16 / V, 512, 1, 3);
-    if constexpr (S < 8) TAKE(16384, V, 16 / V, 1024, 1, 2);
+    TAKE(V, 1, 64 / V, 2, 3, 1);
+    TAKE(V, 1, 128 / V, 2, 3, 1);
+    TAKE(V, 8 / V, 32, 2, 3, 1);
+    TAKE(V, 16 / V, 32, 1, 3, 1);
+    TAKE(V, 16 / V, 64, 1, 3, 1);
+    TAKE(V, 16 / V, 128, 1, 3, 1);
+    TAKE(V, 16 / V, 256, 1, 3, 1);
+    TAKE(V, 16 / V, 512, 1, 3, 1);
+    TAKE(V, 16 / V, 512, 1, 3, 2);
+    TAKE(V, 16 / V, 512, 1, 3, 4);
+    TAKE(V, 16 / V, 512, 1, 3, 8);
   } else {
-    TAKE(8, 1, 1, 8, 1, 4);
-    TAKE(64, 1, 2, 32, 1, 4);
-    TAKE(256, 1, 8, 32, 1, 4);
-    TAKE(512, 1, 16, 32, 1, 3);
-    TAKE(1024, 1, 16, 64, 1, 3);
-    TAKE(2048, 1, 16, 128, 1, 3);
-    TAKE(4096, 1, 16, 256, 1, 3);
-    TAKE(8192, 1, 16, 512, 1, 3);
-    if constexpr (S < 8) TAKE(16384, 1, 16, 1024, 1, 2);
+    TAKE(1, 2, 8, 2, 3, 1);
+    TAKE(1, 2, 32, 2, 3, 1);
+    TAKE(1, 8, 32, 2, 3, 1);
+    TAKE(1, 16, 32, 1, 3, 1);
+    TAKE(1, 16, 64, 1, 3, 1);
+    TAKE(1, 16, 128, 1, 3, 1);
+    TAKE(1, 16, 256, 1, 3, 1);
+    TAKE(1, 16, 512, 1, 3, 1);
+    TAKE(1, 16, 512, 1, 3, 2);
+    TAKE(1, 16, 512, 1, 3, 4);
+    TAKE(1, 16, 512, 1, 3, 8);
   }
 #undef TAKE
   return false;

@@ -1,4 +1,4 @@
-// Layer norm's forward pass for rows that fit the threads of a block: a row is read once, into registers.
+// Layer norm's forward pass for rows that fit the threads of a block or a cluster: a row is read once, into registers.
 #include <algorithm>
 #include <mutex>
 
@@ -7,183 +7,236 @@
 namespace ist {
 namespace {
 
-template <typename XT, typename YT, int V, int NV, int TPR, int RB, int D>
+template <typename XT, typename YT, int V, int NV, int TPR, int RB, int D, int CL, bool FULL>
 __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_forward_kernel(const NormForward a) {
   constexpr int kThreads = TPR > kNormThreads ? TPR : kNormThreads, kSlots = kThreads / TPR, kTile = kSlots * RB;
   constexpr int C = NV * V;
-  constexpr bool kKeep = C <= 16 && RB * C <= 32;          // weight and bias stay in registers
+  constexpr bool kKeep = C <= 16;                          // weight and bias stay in registers
   extern __shared__ __align__(16) char ring[];
-  __shared__ float sh[2 * kThreads / 32 * RB * 2];
+  __shared__ float sh[2 * kThreads / 32 * CL * RB * 2];
   const int t = threadIdx.x % TPR, slot = threadIdx.x / TPR;
-  const int cols = a.cols, room = row_room(cols, sizeof(XT), V == 1);
-  const XT* const x = (const XT*)a.x;
-  YT* const y = (YT*)a.y;
-  const float inv = 1.f / (float)cols;
-  const bool wide = (((uintptr_t)a.weight | (uintptr_t)a.bias) & 15) == 0 && cols % 4 == 0;
-  // tiles of kTile rows of one site; a block takes a run of them
-  const int64_t per_site = ceil_div(a.site_rows, kTile), tiles = per_site * a.sites;
-  const int64_t first = tiles * blockIdx.x / gridDim.x, last = tiles * (blockIdx.x + 1) / gridDim.x;
+  // columns of this block: the row's, or the part of them that is this block's in its cluster
+  const int width = FULL ? TPR * C : part_width(a.cols, CL);
+  const int c0 = CL > 1 ? (int)cluster_rank() * width : 0, cols = CL > 1 ? max(min(a.cols - c0, width), 0) : a.cols;
+  const int room = row_room(width, sizeof(XT), V == 1);
+  const XT* const x = (const XT*)a.x + c0;
+  YT* const y = (YT*)a.y + c0;
+  const float inv = 1.f / (float)a.cols;
+  const bool wide = (((uintptr_t)a.weight | (uintptr_t)a.bias) & 15) == 0 && a.cols % 4 == 0;
+  // tiles of kTile rows of one site; a block (or cluster) takes a run of them
+  const int per_site = (int)ceil_div(a.site_rows, kTile), site_rows = (int)a.site_rows;
+  const int64_t tiles = (int64_t)per_site * a.sites;
+  const int64_t block = blockIdx.x / CL, blocks = gridDim.x / CL;
+  const int64_t begin = tiles * block / blocks;
+  int todo = (int)(tiles * (block + 1) / blocks - begin), to_fetch = todo;
   int turn = 0;
 
-  // row j of this thread's slot in tile k; false if the site has no such row
-  auto row_of = [&](int64_t k, int j, int64_t* r) {
-    const int64_t site = k / per_site, in_site = (k - site * per_site) * kTile + slot * RB + j;
-    *r = site * a.site_rows + in_site;
-    return in_site < a.site_rows;
+  // The slot's rows of a tile: r, r + 1, ..., of which the first `left` are the site's.
+  struct Walk {
+    int site, tile, r, left;
   };
-  auto buffer = [&](int64_t k, int j) { return ring + (((k - first) % D * kSlots + slot) * RB + j) * room; };
-  auto fetch = [&](int64_t k) {
-    if (k < last) {
+  auto start = [&](int64_t k) {
+    Walk w;
+    w.site = (int)(k / per_site);
+    w.tile = (int)(k - (int64_t)w.site * per_site);
+    w.left = site_rows - (w.tile * kTile + slot * RB);
+    w.r = w.site * site_rows + w.tile * kTile + slot * RB;
+    return w;
+  };
+  auto advance = [&](Walk& w) {
+    w.r += kTile;
+    w.left -= kTile;
+    if (++w.tile == per_site) {
+      w.tile = 0;
+      ++w.site;
+      w.left = site_rows - slot * RB;
+      w.r = w.site * site_rows + slot * RB;
+    }
+  };
+  Walk in = start(begin), at = in;
+  int in_stage = 0, stage = 0;
+  auto buffer = [&](int stage, int j) { return ring + ((stage * kSlots + slot) * RB + j) * room; };
+  auto fetch = [&]() {
+    if (to_fetch > 0) {
 #pragma unroll
-      for (int j = 0; j < RB; ++j) {
-        int64_t r;
-        if (row_of(k, j, &r)) fetch_row<XT, V, TPR>(x + r * a.x_ld, cols, buffer(k, j), t);
-      }
+      for (int j = 0; j < RB; ++j)
+        if (j < in.left) fetch_row<XT, V, NV, TPR, FULL>(x + (int64_t)(in.r + j) * a.x_ld, cols, buffer(in_stage, j), t);
+      --to_fetch;
+      advance(in);
+      if (++in_stage == D) in_stage = 0;
     }
     copy_commit();
   };
   uint16_t odd[RB];
-  auto fetch_odd = [&](int64_t k) {
+  auto fetch_odd = [&](const Walk& w) {
 #pragma unroll
-    for (int j = 0; j < RB; ++j) {
-      int64_t r;
-      odd[j] = k < last && row_of(k, j, &r) ? load_odd(x + r * a.x_ld, cols, t) : (uint16_t)0;
-    }
+    for (int j = 0; j < RB; ++j) odd[j] = j < w.left ? load_odd(x + (int64_t)(w.r + j) * a.x_ld, cols, t) : (uint16_t)0;
   };
+  auto here = [&](int i) { return FULL || (t + i * TPR) * V < cols; };
 
   pdl_wait();
   pdl_trigger();
 #pragma unroll
-  for (int k = 0; k < D - 1; ++k) fetch(first + k);
-  if (V == 1) fetch_odd(first);
-  float w[kKeep ? C : 1], b[kKeep ? C : 1];
-  int64_t held = -1;
-  for (int64_t k = first; k < last; ++k) {
-    fetch(k + D - 1);
-    const int64_t site = k / per_site;
-    const float* const ws = a.weight ? a.weight + site * cols : nullptr;
-    const float* const bs = a.bias ? a.bias + site * cols : nullptr;
-    auto vectors = [&](int i, float* wv, float* bv) {
-      const int c = (t + i * TPR) * V;
+  for (int k = 0; k < D - 1; ++k) fetch();
+  if (V == 1 && todo > 0) fetch_odd(at);
+  pair w[kKeep ? C / 2 : 1], b[kKeep ? C / 2 : 1];
+  int held = -1;
+  auto vector = [&](const float* p, int site, float none, int i, float* out) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) { wv[e] = 1.f; bv[e] = 0.f; }
-      if (c < cols) {
-        if (ws) load_vector<V>(ws + c, wide, wv);
-        if (bs) load_vector<V>(bs + c, wide, bv);
-      }
-    };
-    if (kKeep && site != held) {
+    for (int e = 0; e < V; ++e) out[e] = none;
+    if (p && here(i)) load_vector<V>(p + (int64_t)site * a.cols + c0 + (t + i * TPR) * V, wide, out);
+  };
+  for (; todo > 0; --todo) {
+    fetch();
+    if (kKeep && at.site != held) {
+      float f[C];
 #pragma unroll
-      for (int i = 0; i < NV; ++i) vectors(i, w + i * V, b + i * V);
-      held = site;
+      for (int i = 0; i < NV; ++i) vector(a.weight, at.site, 1.f, i, f + i * V);
+#pragma unroll
+      for (int e = 0; e < C / 2; ++e) w[kKeep ? e : 0] = make_pair2(f[2 * e], f[2 * e + 1]);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) vector(a.bias, at.site, 0.f, i, f + i * V);
+#pragma unroll
+      for (int e = 0; e < C / 2; ++e) b[kKeep ? e : 0] = make_pair2(f[2 * e], f[2 * e + 1]);
+      held = at.site;
     }
     copy_wait<D - 1>();
-    int64_t r[RB];
-    bool live[RB];
-#pragma unroll
-    for (int j = 0; j < RB; ++j) live[j] = row_of(k, j, &r[j]);
+    const Walk now = at;
+    advance(at);
     if (V == 1) {
 #pragma unroll
       for (int j = 0; j < RB; ++j)
-        if (live[j]) store_odd(x + r[j] * a.x_ld, cols, buffer(k, j), t, odd[j]);
+        if (j < now.left) store_odd(x + (int64_t)(now.r + j) * a.x_ld, cols, buffer(stage, j), t, odd[j]);
       row_barrier<TPR>();
-      fetch_odd(k + 1);
+      if (todo > 1) fetch_odd(at);
     }
-    float v[RB][C], s[RB];
+    pair v[RB][C / 2];
+    float s[RB];
 #pragma unroll
     for (int j = 0; j < RB; ++j) {
-      const char* const buf = buffer(k, j) + (V == 1 ? (uintptr_t)(x + r[j] * a.x_ld) & 15 : 0);
-      s[j] = 0.f;
+      const char* const buf =
+          buffer(stage, j) + (V == 1 ? (int)((uintptr_t)(x + (int64_t)(now.r + j) * a.x_ld) & 15) : 0) + t * (V * (int)sizeof(XT));
+      float f[C];
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int c = (t + i * TPR) * V;
-        if (c < cols) {
-          unpack<XT, V>(buf + c * sizeof(XT), &v[j][i * V]);
+        if (here(i)) {
+          unpack<XT, V>(buf + i * (TPR * V * sizeof(XT)), f + i * V);
         } else {
 #pragma unroll
-          for (int e = 0; e < V; ++e) v[j][i * V + e] = 0.f;
+          for (int e = 0; e < V; ++e) f[i * V + e] = 0.f;
         }
-#pragma unroll
-        for (int e = 0; e < V; ++e) s[j] += v[j][i * V + e];
       }
+      pair sum = v[j][0] = make_pair2(f[0], f[1]);
+#pragma unroll
+      for (int e = 1; e < C / 2; ++e) {
+        v[j][e] = make_pair2(f[2 * e], f[2 * e + 1]);
+        sum = add(sum, v[j][e]);
+      }
+      s[j] = first(sum) + second(sum);
     }
-    row_sums<TPR, RB>(s, sh, &turn);
+    row_sums<TPR, CL, RB>(s, sh, &turn);
     float q[2 * RB];
 #pragma unroll
     for (int j = 0; j < RB; ++j) {
-      const float mean = s[j] *= inv;
-      float d1 = 0.f, d2 = 0.f;
+      s[j] *= inv;
+      const pair minus = both(-s[j]);
+      pair d1 = both(0.f), d2 = both(0.f);
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const bool in = (t + i * TPR) * V < cols;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float d = in ? v[j][i * V + e] - mean : 0.f;
-          v[j][i * V + e] = d;
-          d1 += d;
-          d2 = fmaf(d, d, d2);
+      for (int e = 0; e < C / 2; ++e) {
+        pair d = add(v[j][e], minus);
+        if (!FULL) {
+          const bool one = here(2 * e / V), two = V == 1 ? here(2 * e + 1) : one;
+          d = make_pair2(one ? first(d) : 0.f, two ? second(d) : 0.f);
         }
+        v[j][e] = d;
+        d1 = add(d1, d);
+        d2 = fma(d, d, d2);
       }
-      q[j] = d1;
-      q[RB + j] = d2;
+      q[j] = first(d1) + second(d1);
+      q[RB + j] = first(d2) + second(d2);
     }
-    row_sums<TPR, 2 * RB>(q, sh, &turn);
-    float rstd[RB], shift[RB];
+    row_sums<TPR, CL, 2 * RB>(q, sh, &turn);
+    pair rstd[RB], shift[RB];
 #pragma unroll
     for (int j = 0; j < RB; ++j) {
       const float rest = q[j] * inv;                        // what rounding left of the mean
       float var = fmaf(-rest, rest, q[RB + j] * inv);
       if (var < 0.f) var = 0.f;                             // a NaN stays one
-      rstd[j] = inverse_root(var + a.eps);
-      shift[j] = -rest * rstd[j];
-      if (live[j] && t == 0) {
-        if (a.mean) a.mean[r[j]] = s[j] + rest;
-        if (a.rstd) a.rstd[r[j]] = rstd[j];
+      const float r = inverse_root(var + a.eps);
+      rstd[j] = both(r);
+      shift[j] = both(-rest * r);
+      if (j < now.left && t == 0 && c0 == 0) {
+        if (a.mean) a.mean[now.r + j] = s[j] + rest;
+        if (a.rstd) a.rstd[now.r + j] = r;
       }
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (t + i * TPR) * V;
-      float wv[V], bv[V];
+      // pairs of this piece; single elements (V = 1) are taken two pieces at a time
+      constexpr int kPairs = V == 1 ? 1 : V / 2;
+      if (V == 1 && i % 2) continue;
+      const int p0 = V == 1 ? i / 2 : i * (V / 2);
+      pair wv[kPairs], bv[kPairs];
       if (kKeep) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) { wv[e] = w[kKeep ? i * V + e : 0]; bv[e] = b[kKeep ? i * V + e : 0]; }
+        for (int e = 0; e < kPairs; ++e) { wv[e] = w[kKeep ? p0 + e : 0]; bv[e] = b[kKeep ? p0 + e : 0]; }
       } else {
-        vectors(i, wv, bv);
+        float f[2 * kPairs], g[2 * kPairs];
+        vector(a.weight, now.site, 1.f, i, f);
+        vector(a.bias, now.site, 0.f, i, g);
+        if (V == 1) {
+          vector(a.weight, now.site, 1.f, i + 1, f + 1);
+          vector(a.bias, now.site, 0.f, i + 1, g + 1);
+        }
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) {
+          wv[e] = make_pair2(f[2 * e], f[2 * e + 1]);
+          bv[e] = make_pair2(g[2 * e], g[2 * e + 1]);
+        }
       }
 #pragma unroll
       for (int j = 0; j < RB; ++j) {
-        float o[V];
+        float o[2 * kPairs];
 #pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = fmaf(fmaf(v[j][i * V + e], rstd[j], shift[j]), wv[e], bv[e]);
-        if (live[j] && c < cols) pack<YT, V>(y + r[j] * a.y_ld + c, o);
+        for (int e = 0; e < kPairs; ++e) {
+          const pair r = fma(fma(v[j][p0 + e], rstd[j], shift[j]), wv[e], bv[e]);
+          o[2 * e] = first(r);
+          o[2 * e + 1] = second(r);
+        }
+        if (j < now.left) {
+          YT* const to = y + (int64_t)(now.r + j) * a.y_ld + t * V;
+          if (here(i)) pack<YT, V>(to + i * (TPR * V), o);
+          if (V == 1 && here(i + 1)) pack<YT, V>(to + (i + 1) * TPR, o + 1);
+        }
       }
     }
+    if (++stage == D) stage = 0;
     if (V == 1) row_barrier<TPR>();                         // the next fetch writes what this tile was read from
   }
   copy_wait<0>();
+  if (CL > 1) cluster_barrier();                            // no block ends while another may write to its sums
 }
 
-template <typename XT, typename YT, int V, int NV, int TPR, int RB, int D>
+template <typename XT, typename YT, int V, int NV, int TPR, int RB, int D, int CL, bool FULL>
 cudaError_t launch(const NormForward& a, cudaStream_t stream) {
   constexpr int kThreads = TPR > kNormThreads ? TPR : kNormThreads, kSlots = kThreads / TPR;
-  const auto kernel = norm_forward_kernel<XT, YT, V, NV, TPR, RB, D>;
-  const int smem = D * kSlots * RB * row_room(a.cols, sizeof(XT), V == 1);
+  const auto kernel = norm_forward_kernel<XT, YT, V, NV, TPR, RB, D, CL, FULL>;
   // the most that any width of this instance asks for, and how many blocks an SM holds then
   constexpr int kMost = D * kSlots * RB * row_room(TPR * V * NV, sizeof(XT), V == 1);
-  static_assert(kMost <= 200 * 1024, "ring too large");
+  static_assert(kMost <= 225 * 1024, "ring too large");
   static std::once_flag once;
   static cudaError_t ready = cudaSuccess;
   static int resident = 1;
   std::call_once(once, [&] {
     ready = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     if (ready == cudaSuccess) ready = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, kThreads, kMost);
-    if (resident < 1) resident = 1;
+    resident = std::max(1, (int)(sm_count() * resident / CL));
   });
   if (ready != cudaSuccess) return ready;
   const int64_t tiles = ceil_div(a.site_rows, kSlots * RB) * a.sites;
-  const int64_t blocks = std::min<int64_t>(tiles, (int64_t)sm_count() * resident);
-  return launch_pdl(kernel, dim3((unsigned)blocks), dim3(kThreads), smem, stream, a);
+  const int64_t blocks = std::min<int64_t>(tiles, resident);
+  const int smem = D * kSlots * RB * row_room(part_width(a.cols, CL), sizeof(XT), V == 1);
+  return launch_rows(kernel, (unsigned)(blocks * CL), kThreads, smem, CL, stream, a);
 }
 
 template <typename XT, typename YT>
@@ -192,27 +245,34 @@ bool dispatch(const NormForward& a, cudaStream_t stream, cudaError_t* e) {
   auto fits = [&](const void* p, int64_t ld, int size) { return (((uintptr_t)p | (uintptr_t)(ld * size)) & (V * size - 1)) == 0; };
   const bool pieces = a.cols % V == 0 && fits(a.x, a.x_ld, sizeof(XT)) && fits(a.y, a.y_ld, sizeof(YT));
   const int n = a.cols;
-#define TAKE(most, v, nv, tpr, rb, d) \
-  if (n <= (most)) return *e = launch<XT, YT, v, nv, tpr, rb, d>(a, stream), true
+#define TAKE(v, nv, tpr, rb, d, cl)                                                                  \
+  if ((v) > 1 && n == (v) * (nv) * (tpr) * (cl))                                                     \
+    return *e = launch<XT, YT, v, nv, tpr, rb, d, cl, (v > 1)>(a, stream), true;                     \
+  if (n <= (v) * (nv) * (tpr) * (cl)) return *e = launch<XT, YT, v, nv, tpr, rb, d, cl, false>(a, stream), true
   if (pieces) {
-    TAKE(64, V, 1, 64 / V, 1, 4);
-    TAKE(128, V, 1, 128 / V, 1, 4);
-    TAKE(256, V, 8 / V, 32, 1, 4);
-    TAKE(512, V, 16 / V, 32, 1, 4);
-    TAKE(1024, V, 32 / V, 32, 1, 3);
-    TAKE(2048, V, 16 / V, 128, 2, 3);
-    TAKE(4096, V, 16 / V, 256, 2, 3);
-    TAKE(8192, V, 16 / V, 512, 1, 3);
-    TAKE(16384, V, 16 / V, 1024, 1, 2);
+    TAKE(V, 1, 64 / V, 4, 3, 1);
+    TAKE(V, 1, 128 / V, 4, 3, 1);
+    TAKE(V, 8 / V, 32, 4, 3, 1);
+    TAKE(V, 16 / V, 32, 2, 3, 1);
+    TAKE(V, 16 / V, 64, 2, 3, 1);
+    TAKE(V, 16 / V, 128, 2, 3, 1);
+    TAKE(V, 16 / V, 256, 2, 3, 1);
+    TAKE(V, 16 / V, 512, 2, 2, 1);
+    TAKE(V, 16 / V, 512, 2, 2, 2);
+    TAKE(V, 16 / V, 512, 2, 2, 4);
+    TAKE(V, 16 / V, 512, 2, 2, 8);
   } else {
-    TAKE(8, 1, 1, 8, 1, 4);
-    TAKE(64, 1, 2, 32, 1, 4);
-    TAKE(256, 1, 8, 32, 1, 4);
-    TAKE(1024, 1, 32, 32, 1, 3);
-    TAKE(2048, 1, 16, 128, 2, 3);
-    TAKE(4096, 1, 16, 256, 2, 3);
-    TAKE(8192, 1, 16, 512, 1, 3);
-    TAKE(16384, 1, 16, 1024, 1, 2);
+    TAKE(1, 2, 8, 4, 3, 1);
+    TAKE(1, 2, 32, 4, 3, 1);
+    TAKE(1, 8, 32, 4, 3, 1);
+    TAKE(1, 16, 32, 2, 3, 1);
+    TAKE(1, 16, 64, 2, 3, 1);
+    TAKE(1, 16, 128, 2, 3, 1);
+    TAKE(1, 16, 256, 2, 3, 1);
+    TAKE(1, 16, 512, 2, 2, 1);
+    TAKE(1, 16, 512, 2, 2, 2);
+    TAKE(1, 16, 512, 2, 2, 4);
+    TAKE(1, 16, 512, 2, 2, 8);
   }
 #undef TAKE
   return false;

@@ -1,10 +1,14 @@
 // What layer norm's two passes share: rows on their way through shared memory, sums over the threads of a row.
 //
-// TPR threads (8 ... 1024) take a row, each NV pieces of V adjacent elements, piece i of thread t being the row's piece
-// t + i TPR.  Rows come in by asynchronous 16- or 8-byte copies, stages ahead of their use.  Where rows are aligned to
-// pieces (V > 1) a thread copies exactly what it reads itself, so no barrier stands between the two.  Rows that start anywhere
-// (V = 1) are copied in 16-byte pieces too, to the same offset from a 16-byte boundary as in memory, and their ends in
-// single elements; then a barrier of the row's threads, and each reads elements TPR apart.
+// TPR threads (8 ... 512) of a block take a row, or its part where a cluster of blocks takes it, each NV pieces of V adjacent
+// elements, piece i of thread t being piece t + i TPR.  Rows come in by asynchronous 16- or 8-byte copies, stages ahead of
+// their use.  Where rows are aligned to pieces (V > 1) a thread copies exactly what it reads itself, so no barrier stands
+// between the two.  Rows that start anywhere (V = 1) are copied in 16-byte pieces too, to the same offset from a 16-byte
+// boundary as in memory, and their ends in single elements; then a barrier of the row's threads, and each reads elements TPR
+// apart.  A thread takes RB rows at a time, whose sums go through the shuffles together.
+//
+// The arithmetic is on pairs of fp32 values (one instruction for two): one by one, issuing instructions took longer than the
+// memory (bf16 rows of 2048, forward: 24 instructions an element, 35 us for 134 MB).
 #pragma once
 
 #include "kernels.h"
@@ -45,7 +49,10 @@ struct NormBackward {
 // norm_forward.cu, norm_backward.cu: false if no kernel takes rows of this width (nothing is launched).
 bool norm_forward_rows(const NormForward& a, bool x_bf16, bool y_bf16, cudaStream_t stream, cudaError_t* e);
 bool norm_backward_rows(const NormBackward& a, bool x_bf16, bool dy_bf16, cudaStream_t stream, cudaError_t* e);
-constexpr int kNormWidest = 16384;     // wider rows have kernels of their own
+constexpr int kNormBlockWidest = 8192, kNormWidest = 8 * kNormBlockWidest;
+// Blocks of a cluster that share a row of the second one.
+inline int norm_cluster(int64_t cols) { return cols <= kNormBlockWidest ? 1 : cols <= 2 * kNormBlockWidest ? 2 : cols <= 4 * kNormBlockWidest ? 4 : 8; }
+     // wider rows have kernels of their own
 
 namespace {
 
@@ -60,6 +67,22 @@ __device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+// Writes to the place in block `rank` of the cluster that corresponds to `at` in this one.
+__device__ __forceinline__ void store_cluster(uint32_t at, uint32_t rank, float v) {
+  uint32_t to;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(at), "r"(rank));
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 
 template <int BYTES> struct Raw;
 template <> struct Raw<2> { typedef uint16_t type; };
@@ -119,16 +142,24 @@ __device__ __forceinline__ void load_vector(const float* p, bool wide, float* v)
   }
 }
 
+// Columns of a block when a row is shared by a cluster of `cl`.
+__host__ __device__ __forceinline__ constexpr int part_width(int cols, int cl) {
+  return cl == 1 ? cols : ((cols + cl - 1) / cl + 7) / 8 * 8;
+}
 // A row's bytes in shared memory: room for its 16-byte pieces, whatever its offset from a boundary.
 __host__ __device__ __forceinline__ constexpr int row_room(int cols, int size, bool anywhere) {
   return (cols * size + 15) / 16 * 16 + (anywhere ? 16 : 0);
 }
 
-// Starts the copies of a row.  Returns the offset of its first element in `buf`.
-template <typename T, int V, int TPR>
+// Starts the copies of a row into `buf`.  FULL: the row has TPR * NV pieces.
+template <typename T, int V, int NV, int TPR, bool FULL>
 __device__ __forceinline__ void fetch_row(const T* row, int cols, char* buf, int t) {
   if (V > 1) {
-    for (int u = t * V; u < cols; u += TPR * V) copy_async<V * sizeof(T)>(shared_address(buf + u * sizeof(T)), row + u);
+    const T* const from = row + t * V;
+    const uint32_t to = shared_address(buf) + t * (V * sizeof(T));
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (FULL || (t + i * TPR) * V < cols) copy_async<V * sizeof(T)>(to + i * (TPR * V * sizeof(T)), from + i * (TPR * V));
   } else {
     const uintptr_t first = (uintptr_t)row, last = first + (uintptr_t)cols * sizeof(T);
     const uintptr_t base = first & ~(uintptr_t)15, whole = (first + 15) & ~(uintptr_t)15, end = last & ~(uintptr_t)15;
@@ -161,38 +192,119 @@ __device__ __forceinline__ void store_odd(const T* row, int cols, char* buf, int
   if (t == 1 && (last & 3)) *reinterpret_cast<uint16_t*>(buf + (last - 2 - base)) = v;
 }
 
-// Sums of N values over the TPR threads of a row, left in all of them; the order is the same on every call.  sh: 2 buffers,
-// used in turn, of [rows of the block][N][warps of a row].
-template <int TPR, int N>
+typedef unsigned long long pair;        // two fp32 values
+__device__ __forceinline__ pair make_pair2(float a, float b) {
+  pair p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(a), "f"(b));
+  return p;
+}
+__device__ __forceinline__ float first(pair p) { return __uint_as_float((uint32_t)p); }
+__device__ __forceinline__ float second(pair p) { return __uint_as_float((uint32_t)(p >> 32)); }
+__device__ __forceinline__ pair both(float a) { return make_pair2(a, a); }
+__device__ __forceinline__ pair add(pair a, pair b) {
+  pair d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ pair mul(pair a, pair b) {
+  pair d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ pair fma(pair a, pair b, pair c) {
+  pair d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+
+constexpr int log2_of(int n) { return n <= 1 ? 0 : 1 + log2_of(n / 2); }
+
+// Sums of N values (a power of two) over the TPR threads of a row and the CL blocks of a cluster, left in all of them; the
+// order is the same on every call.  At each of the first steps a lane keeps half of the values and gives the other half
+// to its partner, so that N values take N - 1 shuffles and one more for each step left, not one per value and step.
+// sh: 2 buffers, used in turn, of [rows of the block][N][warps of a row in the cluster].
+template <int TPR, int CL, int N>
 __device__ __forceinline__ void row_sums(float* v, float* sh, int* turn) {
+  constexpr int L = TPR < 32 ? TPR : 32;                   // lanes of a row within a warp
+  const int lane = threadIdx.x & 31;
+  int n = N, o = L / 2, mine = 0;                          // mine: the value this lane ends with
 #pragma unroll
-  for (int o = (TPR < 32 ? TPR : 32) / 2; o; o >>= 1)
+  for (int s = 0; s < log2_of(N < L ? N : L); ++s, o /= 2) {
+    n /= 2;
+    const bool up = lane & o;
+    mine = mine * 2 + up;
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-  if (TPR > 32) {
-    constexpr int W = TPR / 32;
-    const int row = threadIdx.x / TPR, warp = threadIdx.x % TPR / 32, lane = threadIdx.x & 31;
-    float* const b = sh + *turn * (blockDim.x / 32 * N) + row * N * W;
-    *turn ^= 1;
-    if (lane == 0)
-#pragma unroll
-      for (int i = 0; i < N; ++i) b[i * W + warp] = v[i];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (W <= 8) {
-        float s = b[i * W];
-#pragma unroll
-        for (int w = 1; w < W; ++w) s += b[i * W + w];
-        v[i] = s;
-      } else {
-        float s = lane < W ? b[i * W + lane] : 0.f;
-#pragma unroll
-        for (int o = W / 2; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        v[i] = __shfl_sync(0xffffffffu, s, 0);
-      }
+    for (int i = 0; i < n; ++i) {
+      const float keep = up ? v[i + n] : v[i], give = up ? v[i] : v[i + n];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
     }
   }
+  constexpr int kLeft = N < L ? 1 : N / L;                 // values that a lane has at the end
+#pragma unroll
+  for (; o; o /= 2)
+#pragma unroll
+    for (int i = 0; i < kLeft; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  constexpr int kSteps = log2_of(N < L ? N : L), kShare = L >> kSteps;     // lanes that hold the same values
+  if (TPR <= 32) {
+    if (N > 1) {
+      float r[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) r[i] = __shfl_sync(0xffffffffu, v[i % kLeft], i / kLeft * kShare, L);
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = r[i];
+    }
+    return;
+  }
+  constexpr int W = TPR / 32 * CL;
+  const int row = threadIdx.x / TPR, warp = threadIdx.x % TPR / 32;
+  float* const b = sh + *turn * (blockDim.x / 32 * CL * N) + row * N * W;
+  *turn ^= 1;
+  if (lane % kShare == 0) {
+    if (CL == 1) {
+      b[mine * W + warp] = v[0];
+    } else {
+      const uint32_t at = shared_address(b + mine * W + cluster_rank() * (TPR / 32) + warp);
+#pragma unroll
+      for (int q = 0; q < CL; ++q) store_cluster(at, q, v[0]);
+    }
+  }
+  if (CL == 1) __syncthreads(); else cluster_barrier();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (W <= 8) {
+      float s = b[i * W];
+#pragma unroll
+      for (int w = 1; w < W; ++w) s += b[i * W + w];
+      v[i] = s;
+    } else {
+      float s = lane < W ? b[i * W + lane] : 0.f;
+#pragma unroll
+      for (int w = 32; w < W; w += 32) s += b[i * W + w + lane];
+#pragma unroll
+      for (int o = (W < 32 ? W : 32) / 2; o; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+      v[i] = W < 32 ? __shfl_sync(0xffffffffu, s, 0) : s;
+    }
+  }
+}
+
+// A launch that may start early (see launch_pdl), of clusters of `cluster` blocks.
+template <typename A>
+cudaError_t launch_rows(void (*kernel)(A), unsigned blocks, unsigned threads, size_t smem, unsigned cluster, cudaStream_t stream,
+                        const A& args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args);
 }
 
 template <int TPR>
