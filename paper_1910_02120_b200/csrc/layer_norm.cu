@@ -127,34 +127,57 @@ __global__ void __launch_bounds__(kColumns* kLanes) norm_columns_any_kernel(cons
   }
 }
 
-// dweight and dbias from the parts' sums: 32 columns and 32 lanes of parts to a block, so that all of a column's sums are
-// on their way at once.
-constexpr int kJoinLanes = 32;
-__global__ void __launch_bounds__(kColumns* kJoinLanes) norm_join_kernel(const float* parts_sums, int64_t cols, int sites,
-                                                                        int parts, float* dweight, float* dbias) {
-  __shared__ float sh[kJoinLanes][kColumns + 1];
+// dweight and dbias from the parts' sums.  LANES threads share the parts of four adjacent columns, so that all of a
+// column's sums are on their way at once where there are many parts.  Many blocks of few loads each would be slower than the
+// pass that leaves the sums (8 sites x 9 parts x 16384 columns: 55 us with 32 columns and 32 lanes to a block).
+template <int LANES>
+__global__ void __launch_bounds__(kThreads) norm_join_kernel(const float* parts_sums, int64_t cols, int sites, int parts,
+                                                            float* dweight, float* dbias) {
+  constexpr int kWide = kThreads / LANES * 4;             // columns of a block
+  __shared__ float sh[LANES > 1 ? LANES : 1][kWide];
   pdl_wait();
   pdl_trigger();
   // blocks: [site][dweight, dbias][chunk of columns]
-  const int64_t chunks = ceil_div(cols, kColumns);
-  const int64_t j = (int64_t)(blockIdx.x % chunks) * kColumns + threadIdx.x, which = blockIdx.x / chunks % 2;
+  const int64_t chunks = ceil_div(cols, kWide);
+  const int x = threadIdx.x % (kThreads / LANES), lane = threadIdx.x / (kThreads / LANES);
+  const int64_t first = (int64_t)(blockIdx.x % chunks) * kWide, j = first + x * 4, which = blockIdx.x / chunks % 2;
   const int64_t site = blockIdx.x / (chunks * 2), step = (int64_t)sites * 2 * cols;
   float* const out = which ? dbias : dweight;
   if (!out) return;
-  float s = 0.f;
-  if (j < cols) {
-    const float* in = parts_sums + (site * 2 + which) * cols + j + threadIdx.y * step;
+  const float* in = parts_sums + (site * 2 + which) * cols + j + lane * step;
+  float s[4] = {};
+  if (cols % 4 == 0) {
+    if (j < cols)
 #pragma unroll 4
-    for (int p = threadIdx.y; p < parts; p += kJoinLanes, in += kJoinLanes * step) s += *in;
-  }
-  sh[threadIdx.y][threadIdx.x] = s;
-  __syncthreads();
-  // lane x of warp y: part lane x of column y
-  s = sh[threadIdx.x][threadIdx.y];
+      for (int p = lane; p < parts; p += LANES, in += LANES * step) {
+        float v[4];
+        load4(in, v);
 #pragma unroll
-  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  const int64_t c = (int64_t)(blockIdx.x % chunks) * kColumns + threadIdx.y;
-  if (threadIdx.x == 0 && c < cols) out[site * cols + c] = s;
+        for (int k = 0; k < 4; ++k) s[k] += v[k];
+      }
+  } else {
+#pragma unroll 4
+    for (int p = lane; p < parts; p += LANES, in += LANES * step)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (j + k < cols) s[k] += in[k];
+  }
+  if (LANES == 1) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (j + k < cols) out[site * cols + j + k] = s[k];
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sh[lane][x * 4 + k] = s[k];
+  __syncthreads();
+  for (int c = threadIdx.x; c < kWide; c += kThreads)
+    if (first + c < cols) {
+      float t = 0.f;
+#pragma unroll
+      for (int u = 0; u < LANES; ++u) t += sh[u][c];
+      out[site * cols + first + c] = t;
+    }
 }
 
 // Rows of an array in memory: `rows` runs of `run` bytes, `pitch` bytes apart.
@@ -338,9 +361,16 @@ extern "C" ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, i
                      (const DT*)dy_dev, dy_stride, (const XT*)x_dev, x_stride, cols, site_rows, groups, parts, mean_dev,
                      rstd_dev, part_sums);
   });
-  if (e == cudaSuccess && sums)
-    e = launch_pdl(norm_join_kernel, dim3((unsigned)(chunks * groups * 2)), dim3(kColumns, kJoinLanes), 0, stream,
-                   (const float*)part_sums, cols, groups, parts, dweight_out_dev, dbias_out_dev);
+  if (e == cudaSuccess && sums) {
+    // as many lanes as keep a thread at about eight parts
+    auto blocks = [&](int lanes) { return dim3((unsigned)(ceil_div(cols, kThreads / lanes * 4) * groups * 2)); };
+    auto launch_join = [&](auto kernel, int lanes) {
+      return launch_pdl(kernel, blocks(lanes), dim3(kThreads), 0, stream, (const float*)part_sums, cols, groups, parts,
+                        dweight_out_dev, dbias_out_dev);
+    };
+    e = parts <= 16 ? launch_join(norm_join_kernel<1>, 1) : parts <= 64 ? launch_join(norm_join_kernel<8>, 8)
+                                                                       : launch_join(norm_join_kernel<32>, 32);
+  }
   if (e != cudaSuccess) return fail_call(IST_ERR_CUDA, "ist_layer_norm_backward: %s", cudaGetErrorString(e));
   return IST_OK;
 }

@@ -8,16 +8,20 @@
 namespace ist {
 namespace {
 
+// A tile is gone through twice: first for its sums, then, after the next tile's sums have been begun, for dx.  So the
+// shuffles and the barrier of one tile's sums run beside the arithmetic of another, at the price of unpacking the rows twice
+// (shared memory is not what bounds this) and of two tiles' rows kept.
 template <typename XT, typename DT, int V, int NV, int TPR, int RB, int D, int CL, bool FULL>
 __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_backward_kernel(const NormBackward a) {
   constexpr int kThreads = TPR > kNormThreads ? TPR : kNormThreads, kSlots = kThreads / TPR, kTile = kSlots * RB;
   constexpr int C = NV * V, P = C / 2;
-  extern __shared__ __align__(16) char ring[];
-  __shared__ float sh[2 * kThreads / 32 * CL * RB * 2];
+  static_assert(D >= 3, "two tiles are in use while others arrive");
+  extern __shared__ __align__(128) char ring[];
+  __shared__ RowSums<kThreads, CL, 2 * RB> sh;
   const int t = threadIdx.x % TPR, slot = threadIdx.x / TPR;
   // columns of this block: the row's, or the part of them that is this block's in its cluster
   const int width = FULL ? TPR * C : part_width(a.cols, CL);
-  const int c0 = CL > 1 ? (int)cluster_rank() * width : 0, cols = CL > 1 ? max(min(a.cols - c0, width), 0) : a.cols;
+  const int c0 = CL > 1 ? (int)cluster_ctarank() * width : 0, cols = CL > 1 ? max(min(a.cols - c0, width), 0) : a.cols;
   const int x_room = row_room(width, sizeof(XT), V == 1), room = x_room + row_room(width, sizeof(DT), V == 1);
   const int64_t block = blockIdx.x / CL;
   const int site = (int)(block % a.sites), part = (int)(block / a.sites);
@@ -27,9 +31,15 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
   const XT* const x = (const XT*)a.x + c0;
   const DT* const dy = (const DT*)a.dy + c0;
   const float inv = 1.f / (float)a.cols;
-  int r = begin + slot * RB, in_r = r, stage = 0, in_stage = 0, turn = 0;
+  int r = begin + slot * RB, in_r = r, stage = 0, in_stage = 0;
 
   auto buffer = [&](int stage, int j) { return ring + ((stage * kSlots + slot) * RB + j) * room; };
+  auto x_at = [&](int stage, int j, int r) {
+    return buffer(stage, j) + (V == 1 ? (int)((uintptr_t)(x + (int64_t)(r + j) * a.x_ld) & 15) : 0) + t * (V * (int)sizeof(XT));
+  };
+  auto d_at = [&](int stage, int j, int r) {
+    return buffer(stage, j) + x_room + (V == 1 ? (int)((uintptr_t)(dy + (int64_t)(r + j) * a.dy_ld) & 15) : 0) + t * (V * (int)sizeof(DT));
+  };
   auto fetch = [&]() {
 #pragma unroll
     for (int j = 0; j < RB; ++j)
@@ -57,11 +67,26 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
     }
   };
   auto here = [&](int i) { return FULL || (t + i * TPR) * V < cols; };
+  // kPairs pairs of elements from piece i on: a piece, or two single elements
+  constexpr int kPairs = V == 1 ? 1 : V / 2, kStep = V == 1 ? 2 : 1;
+  auto take = [&](const char* bx, const char* bd, int i, float* xv, float* dv) {
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) {
+      if (here(i + u)) {
+        unpack<XT, V>(bx + (i + u) * (TPR * V * sizeof(XT)), xv + u * V);
+        unpack<DT, V>(bd + (i + u) * (TPR * V * sizeof(DT)), dv + u * V);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) xv[u * V + e] = dv[u * V + e] = 0.f;     // dy = 0 leaves all sums as they are
+      }
+    }
+  };
 
+  Turn turn = begin_sums<CL>(sh);
   pdl_wait();
   pdl_trigger();
 #pragma unroll
-  for (int k = 0; k < D - 1; ++k) fetch();
+  for (int k = 0; k < D - 2; ++k) fetch();
   fetch_more(r);
   pair w[P], aw[P], ab[P];
   {
@@ -81,82 +106,94 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
     }
   }
   const int tiles = (int)ceil_div(end - begin, kTile);
-  for (int k = 0; k < tiles; ++k, r += kTile) {
-    fetch();
-    copy_wait<D - 1>();
-    float rstd[RB];
-    pair minus[RB];
-#pragma unroll
-    for (int j = 0; j < RB; ++j) {
-      minus[j] = both(-next_mean[j]);
-      rstd[j] = next_rstd[j];
-      if (V == 1 && r + j < end) {
-        store_odd(x + (int64_t)(r + j) * a.x_ld, cols, buffer(stage, j), t, odd_x[j]);
-        store_odd(dy + (int64_t)(r + j) * a.dy_ld, cols, buffer(stage, j) + x_room, t, odd_d[j]);
-      }
-    }
-    if (V == 1) row_barrier<TPR>();
-    fetch_more(r + kTile);
-    pair h[RB][P], g[RB][P];
-    float s[2 * RB];
-#pragma unroll
-    for (int j = 0; j < RB; ++j) {
-      const bool live = r + j < end;
-      const char* const bx =
-          buffer(stage, j) + (V == 1 ? (int)((uintptr_t)(x + (int64_t)(r + j) * a.x_ld) & 15) : 0) + t * (V * (int)sizeof(XT));
-      const char* const bd = buffer(stage, j) + x_room +
-                             (V == 1 ? (int)((uintptr_t)(dy + (int64_t)(r + j) * a.dy_ld) & 15) : 0) + t * (V * (int)sizeof(DT));
-      float xv[C], dv[C];
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        if (live && here(i)) {
-          unpack<XT, V>(bx + i * (TPR * V * sizeof(XT)), xv + i * V);
-          unpack<DT, V>(bd + i * (TPR * V * sizeof(DT)), dv + i * V);
-        } else {
-#pragma unroll
-          for (int e = 0; e < V; ++e) xv[i * V + e] = dv[i * V + e] = 0.f;     // dy = 0 leaves all sums as they are
-        }
-      }
-      pair s0 = both(0.f), s1 = both(0.f);
-      const pair rs = both(rstd[j]);
-#pragma unroll
-      for (int e = 0; e < P; ++e) {
-        const pair d = make_pair2(dv[2 * e], dv[2 * e + 1]);
-        h[j][e] = mul(add(make_pair2(xv[2 * e], xv[2 * e + 1]), minus[j]), rs);
-        g[j][e] = mul(d, w[e]);
-        aw[e] = fma(d, h[j][e], aw[e]);
-        ab[e] = add(ab[e], d);
-        s0 = add(s0, g[j][e]);
-        s1 = fma(g[j][e], h[j][e], s1);
-      }
-      s[j] = first(s0) + second(s0);
-      s[RB + j] = first(s1) + second(s1);
-    }
-    if (a.dx) {
-      row_sums<TPR, CL, 2 * RB>(s, sh, &turn);
+  float s[2 * RB], mean[RB], rstd[RB];          // of the tile whose dx is next
+  for (int k = 0; k <= tiles; ++k) {
+    float n[2 * RB], n_mean[RB], n_rstd[RB];    // of the tile whose sums are next
+    if (k < tiles) {
+      fetch();
+      copy_wait<D - 2>();
 #pragma unroll
       for (int j = 0; j < RB; ++j) {
-        if (r + j < end) {
-          const pair m0 = both(-s[j] * inv), m1 = both(-s[RB + j] * inv), rs = both(rstd[j]);
-          XT* const to = (XT*)a.dx + c0 + (int64_t)(r + j) * a.dx_ld + t * V;
-          float o[C];
+        n_mean[j] = next_mean[j];
+        n_rstd[j] = next_rstd[j];
+        if (V == 1 && r + j < end) {
+          store_odd(x + (int64_t)(r + j) * a.x_ld, cols, buffer(stage, j), t, odd_x[j]);
+          store_odd(dy + (int64_t)(r + j) * a.dy_ld, cols, buffer(stage, j) + x_room, t, odd_d[j]);
+        }
+      }
+      if (V == 1) row_barrier<TPR>();
+      fetch_more(r + kTile);
 #pragma unroll
-          for (int e = 0; e < P; ++e) {
-            const pair q = mul(fma(h[j][e], m1, add(g[j][e], m0)), rs);
-            o[2 * e] = first(q);
-            o[2 * e + 1] = second(q);
+      for (int j = 0; j < RB; ++j) {
+        n[j] = n[RB + j] = 0.f;
+        if (r + j >= end) continue;
+        const char *const bx = x_at(stage, j, r), *const bd = d_at(stage, j, r);
+        pair s0 = both(0.f), s1 = both(0.f);
+        const pair rs = both(n_rstd[j]), minus = both(-n_mean[j]);
+#pragma unroll
+        for (int i = 0; i < NV; i += kStep) {
+          float xv[2 * kPairs], dv[2 * kPairs];
+          take(bx, bd, i, xv, dv);
+#pragma unroll
+          for (int e = 0; e < kPairs; ++e) {
+            const int q = i * V / 2 + e;
+            const pair d = make_pair2(dv[2 * e], dv[2 * e + 1]);
+            const pair h = mul(add(make_pair2(xv[2 * e], xv[2 * e + 1]), minus), rs);
+            const pair g = mul(d, w[q]);
+            aw[q] = fma(d, h, aw[q]);
+            ab[q] = add(ab[q], d);
+            s0 = add(s0, g);
+            s1 = fma(g, h, s1);
           }
+        }
+        n[j] = first(s0) + second(s0);
+        n[RB + j] = first(s1) + second(s1);
+      }
+      if (a.dx) begin_row_sums<TPR, CL, 2 * RB>(n, sh, turn);
+    }
+    if (k > 0 && a.dx) {
+      const int old = stage ? stage - 1 : D - 1, o_r = r - kTile;
 #pragma unroll
-          for (int i = 0; i < NV; ++i)
-            if (here(i)) pack<XT, V>(to + i * (TPR * V), o + i * V);
+      for (int j = 0; j < RB; ++j) {
+        if (o_r + j < end) {
+          const char *const bx = x_at(old, j, o_r), *const bd = d_at(old, j, o_r);
+          const pair m0 = both(-s[j] * inv), m1 = both(-s[RB + j] * inv), rs = both(rstd[j]), minus = both(-mean[j]);
+          XT* const to = (XT*)a.dx + c0 + (int64_t)(o_r + j) * a.dx_ld + t * V;
+#pragma unroll
+          for (int i = 0; i < NV; i += kStep) {
+            float xv[2 * kPairs], dv[2 * kPairs];
+            take(bx, bd, i, xv, dv);
+#pragma unroll
+            for (int e = 0; e < kPairs; ++e) {
+              const int q = i * V / 2 + e;
+              const pair h = mul(add(make_pair2(xv[2 * e], xv[2 * e + 1]), minus), rs);
+              const pair o = mul(fma(h, m1, fma(make_pair2(dv[2 * e], dv[2 * e + 1]), w[q], m0)), rs);
+              xv[2 * e] = first(o);
+              xv[2 * e + 1] = second(o);
+            }
+#pragma unroll
+            for (int u = 0; u < kStep; ++u)
+              if (here(i + u)) pack<XT, V>(to + (i + u) * (TPR * V), xv + u * V);
+          }
         }
       }
     }
-    if (++stage == D) stage = 0;
-    if (V == 1) row_barrier<TPR>();                         // the next fetch writes what this tile was read from
+    if (V == 1) row_barrier<TPR>();                         // the next fetch writes what the older tile was read from
+    if (k < tiles) {
+      if (a.dx) end_row_sums<TPR, CL, 2 * RB>(n, sh, &turn);
+#pragma unroll
+      for (int j = 0; j < RB; ++j) {
+        s[j] = n[j];
+        s[RB + j] = n[RB + j];
+        mean[j] = n_mean[j];
+        rstd[j] = n_rstd[j];
+      }
+      if (++stage == D) stage = 0;
+      r += kTile;
+    }
   }
   copy_wait<0>();
-  if (CL > 1) cluster_barrier();                            // no block ends while another may write to its sums
+  if (CL > 1) cluster_sync_all();                           // no block ends while another may write to its sums
   if (!a.wsum && !a.bsum) return;
   const int64_t at = ((int64_t)part * a.sites + site) * a.sum_ld + c0;
   // the slots' sums are joined in shared memory, slot after slot
@@ -216,30 +253,32 @@ bool dispatch(const NormBackward& a, cudaStream_t stream, cudaError_t* e) {
   if ((v) > 1 && n == (v) * (nv) * (tpr) * (cl))                                                     \
     return *e = launch<XT, DT, v, nv, tpr, rb, d, cl, (v > 1)>(a, stream), true;                     \
   if (n <= (v) * (nv) * (tpr) * (cl)) return *e = launch<XT, DT, v, nv, tpr, rb, d, cl, false>(a, stream), true
+  // two tiles in use and one or two on their way, in the shared memory of two blocks (or one of 512 threads)
+  constexpr int D = sizeof(XT) + sizeof(DT) == 8 ? 3 : 4;
   if (pieces) {
-    TAKE(V, 1, 64 / V, 2, 3, 1);
-    TAKE(V, 1, 128 / V, 2, 3, 1);
-    TAKE(V, 8 / V, 32, 2, 3, 1);
-    TAKE(V, 16 / V, 32, 1, 3, 1);
-    TAKE(V, 16 / V, 64, 1, 3, 1);
-    TAKE(V, 16 / V, 128, 1, 3, 1);
-    TAKE(V, 16 / V, 256, 1, 3, 1);
-    TAKE(V, 16 / V, 512, 1, 3, 1);
-    TAKE(V, 16 / V, 512, 1, 3, 2);
-    TAKE(V, 16 / V, 512, 1, 3, 4);
-    TAKE(V, 16 / V, 512, 1, 3, 8);
+    TAKE(V, 1, 64 / V, 2, 4, 1);
+    TAKE(V, 1, 128 / V, 2, 4, 1);
+    TAKE(V, 8 / V, 32, 2, 4, 1);
+    TAKE(V, 16 / V, 32, 1, D, 1);
+    TAKE(V, 16 / V, 64, 1, D, 1);
+    TAKE(V, 16 / V, 128, 1, D, 1);
+    TAKE(V, 16 / V, 256, 1, D, 1);
+    TAKE(V, 16 / V, 512, 1, D, 1);
+    TAKE(V, 16 / V, 512, 1, D, 2);
+    TAKE(V, 16 / V, 512, 1, D, 4);
+    TAKE(V, 16 / V, 512, 1, D, 8);
   } else {
-    TAKE(1, 2, 8, 2, 3, 1);
-    TAKE(1, 2, 32, 2, 3, 1);
-    TAKE(1, 8, 32, 2, 3, 1);
-    TAKE(1, 16, 32, 1, 3, 1);
-    TAKE(1, 16, 64, 1, 3, 1);
-    TAKE(1, 16, 128, 1, 3, 1);
-    TAKE(1, 16, 256, 1, 3, 1);
-    TAKE(1, 16, 512, 1, 3, 1);
-    TAKE(1, 16, 512, 1, 3, 2);
-    TAKE(1, 16, 512, 1, 3, 4);
-    TAKE(1, 16, 512, 1, 3, 8);
+    TAKE(1, 2, 8, 2, 4, 1);
+    TAKE(1, 2, 32, 2, 4, 1);
+    TAKE(1, 8, 32, 2, 4, 1);
+    TAKE(1, 16, 32, 1, D, 1);
+    TAKE(1, 16, 64, 1, D, 1);
+    TAKE(1, 16, 128, 1, D, 1);
+    TAKE(1, 16, 256, 1, D, 1);
+    TAKE(1, 16, 512, 1, D, 1);
+    TAKE(1, 16, 512, 1, D, 2);
+    TAKE(1, 16, 512, 1, D, 4);
+    TAKE(1, 16, 512, 1, D, 8);
   }
 #undef TAKE
   return false;

@@ -11,13 +11,13 @@ template <typename XT, typename YT, int V, int NV, int TPR, int RB, int D, int C
 __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_forward_kernel(const NormForward a) {
   constexpr int kThreads = TPR > kNormThreads ? TPR : kNormThreads, kSlots = kThreads / TPR, kTile = kSlots * RB;
   constexpr int C = NV * V;
-  constexpr bool kKeep = C <= 16;                          // weight and bias stay in registers
-  extern __shared__ __align__(16) char ring[];
-  __shared__ float sh[2 * kThreads / 32 * CL * RB * 2];
+  constexpr bool kKeep = C * (RB + 2) <= 96;               // weight and bias stay in registers
+  extern __shared__ __align__(128) char ring[];
+  __shared__ RowSums<kThreads, CL, 2 * RB> sh;
   const int t = threadIdx.x % TPR, slot = threadIdx.x / TPR;
   // columns of this block: the row's, or the part of them that is this block's in its cluster
   const int width = FULL ? TPR * C : part_width(a.cols, CL);
-  const int c0 = CL > 1 ? (int)cluster_rank() * width : 0, cols = CL > 1 ? max(min(a.cols - c0, width), 0) : a.cols;
+  const int c0 = CL > 1 ? (int)cluster_ctarank() * width : 0, cols = CL > 1 ? max(min(a.cols - c0, width), 0) : a.cols;
   const int room = row_room(width, sizeof(XT), V == 1);
   const XT* const x = (const XT*)a.x + c0;
   YT* const y = (YT*)a.y + c0;
@@ -29,7 +29,6 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
   const int64_t block = blockIdx.x / CL, blocks = gridDim.x / CL;
   const int64_t begin = tiles * block / blocks;
   int todo = (int)(tiles * (block + 1) / blocks - begin), to_fetch = todo;
-  int turn = 0;
 
   // The slot's rows of a tile: r, r + 1, ..., of which the first `left` are the site's.
   struct Walk {
@@ -74,6 +73,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
   };
   auto here = [&](int i) { return FULL || (t + i * TPR) * V < cols; };
 
+  Turn turn = begin_sums<CL>(sh);
   pdl_wait();
   pdl_trigger();
 #pragma unroll
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
     if (V == 1) row_barrier<TPR>();                         // the next fetch writes what this tile was read from
   }
   copy_wait<0>();
-  if (CL > 1) cluster_barrier();                            // no block ends while another may write to its sums
+  if (CL > 1) cluster_sync_all();                           // no block ends while another may write to its sums
 }
 
 template <typename XT, typename YT, int V, int NV, int TPR, int RB, int D, int CL, bool FULL>
@@ -258,9 +258,9 @@ bool dispatch(const NormForward& a, cudaStream_t stream, cudaError_t* e) {
     TAKE(V, 16 / V, 128, 2, 3, 1);
     TAKE(V, 16 / V, 256, 2, 3, 1);
     TAKE(V, 16 / V, 512, 2, 2, 1);
-    TAKE(V, 16 / V, 512, 2, 2, 2);
-    TAKE(V, 16 / V, 512, 2, 2, 4);
-    TAKE(V, 16 / V, 512, 2, 2, 8);
+    TAKE(V, 32 / V, 512, 1, 3, 1);
+    TAKE(V, 32 / V, 512, 1, 3, 2);
+    TAKE(V, 32 / V, 512, 1, 3, 4);
   } else {
     TAKE(1, 2, 8, 4, 3, 1);
     TAKE(1, 2, 32, 4, 3, 1);
@@ -270,9 +270,9 @@ bool dispatch(const NormForward& a, cudaStream_t stream, cudaError_t* e) {
     TAKE(1, 16, 128, 2, 3, 1);
     TAKE(1, 16, 256, 2, 3, 1);
     TAKE(1, 16, 512, 2, 2, 1);
-    TAKE(1, 16, 512, 2, 2, 2);
-    TAKE(1, 16, 512, 2, 2, 4);
-    TAKE(1, 16, 512, 2, 2, 8);
+    TAKE(1, 32, 512, 1, 3, 1);
+    TAKE(1, 32, 512, 1, 3, 2);
+    TAKE(1, 32, 512, 1, 3, 4);
   }
 #undef TAKE
   return false;

@@ -12,6 +12,7 @@
 #pragma once
 
 #include "kernels.h"
+#include "tc_ptx.cuh"
 
 namespace ist {
 
@@ -49,14 +50,12 @@ struct NormBackward {
 // norm_forward.cu, norm_backward.cu: false if no kernel takes rows of this width (nothing is launched).
 bool norm_forward_rows(const NormForward& a, bool x_bf16, bool y_bf16, cudaStream_t stream, cudaError_t* e);
 bool norm_backward_rows(const NormBackward& a, bool x_bf16, bool dy_bf16, cudaStream_t stream, cudaError_t* e);
-constexpr int kNormBlockWidest = 8192, kNormWidest = 8 * kNormBlockWidest;
+constexpr int kNormWidest = 65536;
 // Blocks of a cluster that share a row of the second one.
-inline int norm_cluster(int64_t cols) { return cols <= kNormBlockWidest ? 1 : cols <= 2 * kNormBlockWidest ? 2 : cols <= 4 * kNormBlockWidest ? 4 : 8; }
-     // wider rows have kernels of their own
+inline int norm_cluster(int64_t cols) { return cols <= 8192 ? 1 : cols <= 16384 ? 2 : cols <= 32768 ? 4 : 8; }
 
 namespace {
 
-__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 template <int BYTES>
 __device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
   if (BYTES == 16)
@@ -68,20 +67,12 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-// Writes to the place in block `rank` of the cluster that corresponds to `at` in this one.
-__device__ __forceinline__ void store_cluster(uint32_t at, uint32_t rank, float v) {
-  uint32_t to;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(at), "r"(rank));
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(v) : "memory");
-}
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+// Writes to the place in block `rank` of the cluster that corresponds to `at` in this one; the write itself tells that block's
+// barrier, so no fence stands behind it (a cluster barrier would wait for all of the threads' stores to global memory too:
+// rows of 16384 took 150 us that way and TODO us this way).
+__device__ __forceinline__ void send_cluster(float* at, uint64_t* bar, uint32_t rank, float v) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];"
+               ::"r"(map_to_cta(at, rank)), "f"(v), "r"(map_to_cta(bar, rank)) : "memory");
 }
 
 template <int BYTES> struct Raw;
@@ -146,9 +137,10 @@ __device__ __forceinline__ void load_vector(const float* p, bool wide, float* v)
 __host__ __device__ __forceinline__ constexpr int part_width(int cols, int cl) {
   return cl == 1 ? cols : ((cols + cl - 1) / cl + 7) / 8 * 8;
 }
-// A row's bytes in shared memory: room for its 16-byte pieces, whatever its offset from a boundary.
+// A row's bytes in shared memory: room for its 16-byte pieces, whatever its offset from a boundary, in whole lines of 128
+// bytes (a warp's access that starts inside a line takes one turn more: fp32 rows of 1024, forward, 33 us and 39 us).
 __host__ __device__ __forceinline__ constexpr int row_room(int cols, int size, bool anywhere) {
-  return (cols * size + 15) / 16 * 16 + (anywhere ? 16 : 0);
+  return (cols * size + (anywhere ? 15 : 0) + 127) / 128 * 128;
 }
 
 // Starts the copies of a row into `buf`.  FULL: the row has TPR * NV pieces.
@@ -156,7 +148,7 @@ template <typename T, int V, int NV, int TPR, bool FULL>
 __device__ __forceinline__ void fetch_row(const T* row, int cols, char* buf, int t) {
   if (V > 1) {
     const T* const from = row + t * V;
-    const uint32_t to = shared_address(buf) + t * (V * sizeof(T));
+    const uint32_t to = smem_u32(buf) + t * (V * sizeof(T));
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (FULL || (t + i * TPR) * V < cols) copy_async<V * sizeof(T)>(to + i * (TPR * V * sizeof(T)), from + i * (TPR * V));
@@ -164,15 +156,15 @@ __device__ __forceinline__ void fetch_row(const T* row, int cols, char* buf, int
     const uintptr_t first = (uintptr_t)row, last = first + (uintptr_t)cols * sizeof(T);
     const uintptr_t base = first & ~(uintptr_t)15, whole = (first + 15) & ~(uintptr_t)15, end = last & ~(uintptr_t)15;
     for (uintptr_t p = whole + 16 * t; p + 16 <= end; p += 16 * TPR)
-      copy_async<16>(shared_address(buf + (p - base)), reinterpret_cast<const void*>(p));
+      copy_async<16>(smem_u32(buf + (p - base)), reinterpret_cast<const void*>(p));
     // the ends, in fp32 words; single bf16 elements among them are left to fetch_odd
     const uintptr_t head = whole < last ? whole : last;          // a short row may lie between two boundaries
     const uintptr_t word = (first + 3) & ~(uintptr_t)3;
     for (uintptr_t p = word + 4 * t; p + 4 <= head; p += 4 * TPR)
-      copy_async<4>(shared_address(buf + (p - base)), reinterpret_cast<const void*>(p));
+      copy_async<4>(smem_u32(buf + (p - base)), reinterpret_cast<const void*>(p));
     if (end >= whole)
       for (uintptr_t p = end + 4 * t; p + 4 <= last; p += 4 * TPR)
-        copy_async<4>(shared_address(buf + (p - base)), reinterpret_cast<const void*>(p));
+        copy_async<4>(smem_u32(buf + (p - base)), reinterpret_cast<const void*>(p));
   }
 }
 // bf16 rows that start or end in the middle of a 4-byte word: thread 0 and thread 1 of the row carry those elements.
@@ -222,9 +214,33 @@ constexpr int log2_of(int n) { return n <= 1 ? 0 : 1 + log2_of(n / 2); }
 // Sums of N values (a power of two) over the TPR threads of a row and the CL blocks of a cluster, left in all of them; the
 // order is the same on every call.  At each of the first steps a lane keeps half of the values and gives the other half
 // to its partner, so that N values take N - 1 shuffles and one more for each step left, not one per value and step.
-// sh: 2 buffers, used in turn, of [rows of the block][N][warps of a row in the cluster].
-template <int TPR, int CL, int N>
-__device__ __forceinline__ void row_sums(float* v, float* sh, int* turn) {
+// RowSums: 2 buffers, used in turn, of [rows of the block][N][warps of a row in the cluster], N up to MOST.  A thread that
+// writes a buffer again has read the sums of the use in between, to which every thread of the row contributed after reading
+// this one, so one barrier per use is enough.  A wait for other blocks' sums that does not end makes them NaN.
+template <int THREADS, int CL, int MOST>
+struct RowSums {
+  float part[2 * (THREADS / 32) * CL * MOST];
+  uint64_t bar[CL > 1 ? 2 : 1];
+};
+struct Turn {
+  int buffer, parity;
+  bool gave_up;
+};
+template <int CL, typename S>
+__device__ __forceinline__ Turn begin_sums(S& sh) {
+  if (CL > 1) {
+    if (threadIdx.x == 0) {
+      mbar_init(&sh.bar[0], 1);
+      mbar_init(&sh.bar[CL > 1 ? 1 : 0], 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    cluster_sync_all();
+  }
+  return Turn{0, 0, false};
+}
+// The sums' first half: everything up to where other warps' values are needed.
+template <int TPR, int CL, int N, typename S>
+__device__ __forceinline__ void begin_row_sums(float* v, S& sh, const Turn& turn) {
   constexpr int L = TPR < 32 ? TPR : 32;                   // lanes of a row within a warp
   const int lane = threadIdx.x & 31;
   int n = N, o = L / 2, mine = 0;                          // mine: the value this lane ends with
@@ -257,18 +273,39 @@ __device__ __forceinline__ void row_sums(float* v, float* sh, int* turn) {
   }
   constexpr int W = TPR / 32 * CL;
   const int row = threadIdx.x / TPR, warp = threadIdx.x % TPR / 32;
-  float* const b = sh + *turn * (blockDim.x / 32 * CL * N) + row * N * W;
-  *turn ^= 1;
-  if (lane % kShare == 0) {
-    if (CL == 1) {
-      b[mine * W + warp] = v[0];
-    } else {
-      const uint32_t at = shared_address(b + mine * W + cluster_rank() * (TPR / 32) + warp);
+  float* const b = sh.part + turn.buffer * (sizeof(sh.part) / 8) + row * N * W;
+  if (CL == 1) {
+    if (lane % kShare == 0) b[mine * W + warp] = v[0];
+  } else {
+    uint64_t* const bar = &sh.bar[turn.buffer];
+    if (threadIdx.x == 0) mbar_expect_tx(bar, W * N * sizeof(float));
+    if (lane % kShare == 0)
 #pragma unroll
-      for (int q = 0; q < CL; ++q) store_cluster(at, q, v[0]);
-    }
+      for (int q = 0; q < CL; ++q) send_cluster(b + mine * W + cluster_ctarank() * (TPR / 32) + warp, bar, q, v[0]);
   }
-  if (CL == 1) __syncthreads(); else cluster_barrier();
+}
+// Their second half: waits for the other warps and adds.
+template <int TPR, int CL, int N, typename S>
+__device__ __forceinline__ void end_row_sums(float* v, S& sh, Turn* turn) {
+  if (TPR <= 32) return;
+  constexpr int W = TPR / 32 * CL;
+  const int row = threadIdx.x / TPR, lane = threadIdx.x & 31;
+  const float* const b = sh.part + turn->buffer * (sizeof(sh.part) / 8) + row * N * W;
+  if (CL == 1) {
+    __syncthreads();
+  } else {
+    uint64_t* const bar = &sh.bar[turn->buffer];
+    if (!turn->gave_up && !mbar_try_wait<true>(bar, turn->parity)) {
+      const long long begin = clock64();
+      while (!mbar_try_wait<true>(bar, turn->parity))
+        if (clock64() - begin > kWaitLimitCycles) {
+          turn->gave_up = true;
+          break;
+        }
+    }
+    turn->parity ^= turn->buffer;          // the barrier's next use has the other parity
+  }
+  turn->buffer ^= 1;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     if (W <= 8) {
@@ -284,7 +321,14 @@ __device__ __forceinline__ void row_sums(float* v, float* sh, int* turn) {
       for (int o = (W < 32 ? W : 32) / 2; o; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
       v[i] = W < 32 ? __shfl_sync(0xffffffffu, s, 0) : s;
     }
+    if (CL > 1 && turn->gave_up) v[i] = __uint_as_float(0x7fc00000u);
   }
+}
+
+template <int TPR, int CL, int N, typename S>
+__device__ __forceinline__ void row_sums(float* v, S& sh, Turn* turn) {
+  begin_row_sums<TPR, CL, N>(v, sh, *turn);
+  end_row_sums<TPR, CL, N>(v, sh, turn);
 }
 
 // A launch that may start early (see launch_pdl), of clusters of `cluster` blocks.
