@@ -224,7 +224,7 @@ int parts_of(int64_t rows, int64_t cols, int groups) {
   const int64_t site_rows = rows / groups;
   int64_t parts, least;
   if (cols <= kNormWidest) {
-    parts = (int64_t)sm_count() * (cols <= 4096 ? 2 : 1) / norm_cluster(cols) / groups;
+    parts = (int64_t)sm_count() * (cols <= 256 ? 2 : 1) / norm_cluster(cols) / groups;
     least = ceil_div(16384, cols);
   } else {
     parts = ceil_div((int64_t)sm_count() * 8, ceil_div(cols, kColumns) * groups);

@@ -11,10 +11,11 @@ namespace {
 // A tile is gone through twice: first for its sums, then, after the next tile's sums have been begun, for dx.  So the
 // shuffles and the barrier of one tile's sums run beside the arithmetic of another, at the price of unpacking the rows twice
 // (shared memory is not what bounds this) and of two tiles' rows kept.
-template <typename XT, typename DT, int V, int NV, int TPR, int RB, int D, int CL, bool FULL>
-__global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_backward_kernel(const NormBackward a) {
-  constexpr int kThreads = TPR > kNormThreads ? TPR : kNormThreads, kSlots = kThreads / TPR, kTile = kSlots * RB;
+template <typename XT, typename DT, int V, int NV, int TPR, int RB, int D, int CL, int LEAST>
+__global__ void __launch_bounds__(NV * V == 16 ? 512 : kNormThreads) norm_backward_kernel(const NormBackward a) {
+  constexpr int kThreads = NV * V == 16 ? 512 : kNormThreads, kSlots = kThreads / TPR, kTile = kSlots * RB;
   constexpr int C = NV * V, P = C / 2;
+  constexpr bool FULL = LEAST == TPR * C;                  // of a block's columns: no piece is missing
   static_assert(D >= 3, "two tiles are in use while others arrive");
   extern __shared__ __align__(128) char ring[];
   __shared__ RowSums<kThreads, CL, 2 * RB> sh;
@@ -44,8 +45,8 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
 #pragma unroll
     for (int j = 0; j < RB; ++j)
       if (in_r + j < end) {
-        fetch_row<XT, V, NV, TPR, FULL>(x + (int64_t)(in_r + j) * a.x_ld, cols, buffer(in_stage, j), t);
-        fetch_row<DT, V, NV, TPR, FULL>(dy + (int64_t)(in_r + j) * a.dy_ld, cols, buffer(in_stage, j) + x_room, t);
+        fetch_row<XT, V, NV, TPR, LEAST>(x + (int64_t)(in_r + j) * a.x_ld, cols, buffer(in_stage, j), t);
+        fetch_row<DT, V, NV, TPR, LEAST>(dy + (int64_t)(in_r + j) * a.dy_ld, cols, buffer(in_stage, j) + x_room, t);
       }
     in_r += kTile;
     if (++in_stage == D) in_stage = 0;
@@ -66,7 +67,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
       }
     }
   };
-  auto here = [&](int i) { return FULL || (t + i * TPR) * V < cols; };
+  auto here = [&](int i) { return (i + 1) * TPR * V <= LEAST || (t + i * TPR) * V < cols; };
   // kPairs pairs of elements from piece i on: a piece, or two single elements
   constexpr int kPairs = V == 1 ? 1 : V / 2, kStep = V == 1 ? 2 : 1;
   auto take = [&](const char* bx, const char* bd, int i, float* xv, float* dv) {
@@ -227,10 +228,10 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
   }
 }
 
-template <typename XT, typename DT, int V, int NV, int TPR, int RB, int D, int CL, bool FULL>
+template <typename XT, typename DT, int V, int NV, int TPR, int RB, int D, int CL, int LEAST>
 cudaError_t launch(const NormBackward& a, cudaStream_t stream) {
-  constexpr int kThreads = TPR > kNormThreads ? TPR : kNormThreads, kSlots = kThreads / TPR;
-  const auto kernel = norm_backward_kernel<XT, DT, V, NV, TPR, RB, D, CL, FULL>;
+  constexpr int kThreads = NV * V == 16 ? 512 : kNormThreads, kSlots = kThreads / TPR;
+  const auto kernel = norm_backward_kernel<XT, DT, V, NV, TPR, RB, D, CL, LEAST>;
   auto ring = [](int cols) { return D * kSlots * RB * (row_room(cols, sizeof(XT), V == 1) + row_room(cols, sizeof(DT), V == 1)); };
   constexpr int kJoin = kSlots > 1 ? kSlots * 2 * NV * V * TPR * 4 : 0;
   constexpr int kMost = std::max(kJoin, D * kSlots * RB * (row_room(TPR * V * NV, sizeof(XT), V == 1) + row_room(TPR * V * NV, sizeof(DT), V == 1)));
@@ -249,36 +250,37 @@ bool dispatch(const NormBackward& a, cudaStream_t stream, cudaError_t* e) {
   const bool pieces = a.cols % V == 0 && fits(a.x, a.x_ld, sizeof(XT)) && fits(a.dy, a.dy_ld, sizeof(DT)) &&
                       (!a.dx || fits(a.dx, a.dx_ld, sizeof(XT)));
   const int n = a.cols;
-#define TAKE(v, nv, tpr, rb, d, cl)                                                                  \
-  if ((v) > 1 && n == (v) * (nv) * (tpr) * (cl))                                                     \
-    return *e = launch<XT, DT, v, nv, tpr, rb, d, cl, (v > 1)>(a, stream), true;                     \
-  if (n <= (v) * (nv) * (tpr) * (cl)) return *e = launch<XT, DT, v, nv, tpr, rb, d, cl, false>(a, stream), true
+  // least: columns that are too many for the line before; of a cluster's block, which may have as little as none, 0
+#define TAKE(least, v, nv, tpr, rb, d, cl)                                                                  \
+  if ((v) > 1 && n == (v) * (nv) * (tpr) * (cl))                                                           \
+    return *e = launch<XT, DT, v, nv, tpr, rb, d, cl, (v) * (nv) * (tpr)>(a, stream), true;               \
+  if (n <= (v) * (nv) * (tpr) * (cl)) return *e = launch<XT, DT, v, nv, tpr, rb, d, cl, least>(a, stream), true
   // two tiles in use and one or two on their way, in the shared memory of two blocks (or one of 512 threads)
-  constexpr int D = sizeof(XT) + sizeof(DT) == 8 ? 3 : 4;
+  constexpr int S = sizeof(XT) + sizeof(DT), D = S == 6 ? 4 : 3, R = S == 4 ? 2 : 1;
   if (pieces) {
-    TAKE(V, 1, 64 / V, 2, 4, 1);
-    TAKE(V, 1, 128 / V, 2, 4, 1);
-    TAKE(V, 8 / V, 32, 2, 4, 1);
-    TAKE(V, 16 / V, 32, 1, D, 1);
-    TAKE(V, 16 / V, 64, 1, D, 1);
-    TAKE(V, 16 / V, 128, 1, D, 1);
-    TAKE(V, 16 / V, 256, 1, D, 1);
-    TAKE(V, 16 / V, 512, 1, D, 1);
-    TAKE(V, 16 / V, 512, 1, D, 2);
-    TAKE(V, 16 / V, 512, 1, D, 4);
-    TAKE(V, 16 / V, 512, 1, D, 8);
+    TAKE(0, V, 1, 64 / V, 4, 3, 1);
+    TAKE(65, V, 1, 128 / V, 4, 3, 1);
+    TAKE(129, V, 8 / V, 32, 4, 3, 1);
+    TAKE(257, V, 16 / V, 32, R, D, 1);
+    TAKE(513, V, 16 / V, 64, R, D, 1);
+    TAKE(1025, V, 16 / V, 128, R, D, 1);
+    TAKE(2049, V, 16 / V, 256, R, D, 1);
+    TAKE(4097, V, 16 / V, 512, R, D, 1);
+    TAKE(0, V, 16 / V, 512, R, D, 2);
+    TAKE(0, V, 16 / V, 512, R, D, 4);
+    TAKE(0, V, 16 / V, 512, R, D, 8);
   } else {
-    TAKE(1, 2, 8, 2, 4, 1);
-    TAKE(1, 2, 32, 2, 4, 1);
-    TAKE(1, 8, 32, 2, 4, 1);
-    TAKE(1, 16, 32, 1, D, 1);
-    TAKE(1, 16, 64, 1, D, 1);
-    TAKE(1, 16, 128, 1, D, 1);
-    TAKE(1, 16, 256, 1, D, 1);
-    TAKE(1, 16, 512, 1, D, 1);
-    TAKE(1, 16, 512, 1, D, 2);
-    TAKE(1, 16, 512, 1, D, 4);
-    TAKE(1, 16, 512, 1, D, 8);
+    TAKE(0, 1, 2, 8, 4, 3, 1);
+    TAKE(17, 1, 2, 32, 4, 3, 1);
+    TAKE(65, 1, 8, 32, 4, 3, 1);
+    TAKE(257, 1, 16, 32, R, D, 1);
+    TAKE(513, 1, 16, 64, R, D, 1);
+    TAKE(1025, 1, 16, 128, R, D, 1);
+    TAKE(2049, 1, 16, 256, R, D, 1);
+    TAKE(4097, 1, 16, 512, R, D, 1);
+    TAKE(0, 1, 16, 512, R, D, 2);
+    TAKE(0, 1, 16, 512, R, D, 4);
+    TAKE(0, 1, 16, 512, R, D, 8);
   }
 #undef TAKE
   return false;

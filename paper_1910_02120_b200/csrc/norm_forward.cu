@@ -7,10 +7,11 @@
 namespace ist {
 namespace {
 
-template <typename XT, typename YT, int V, int NV, int TPR, int RB, int D, int CL, bool FULL>
+template <typename XT, typename YT, int V, int NV, int TPR, int RB, int D, int CL, int LEAST>
 __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_forward_kernel(const NormForward a) {
   constexpr int kThreads = TPR > kNormThreads ? TPR : kNormThreads, kSlots = kThreads / TPR, kTile = kSlots * RB;
   constexpr int C = NV * V;
+  constexpr bool FULL = LEAST == TPR * C;                  // of a block's columns: no piece is missing
   constexpr bool kKeep = C * (RB + 2) <= 96;               // weight and bias stay in registers
   extern __shared__ __align__(128) char ring[];
   __shared__ RowSums<kThreads, CL, 2 * RB> sh;
@@ -59,7 +60,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
     if (to_fetch > 0) {
 #pragma unroll
       for (int j = 0; j < RB; ++j)
-        if (j < in.left) fetch_row<XT, V, NV, TPR, FULL>(x + (int64_t)(in.r + j) * a.x_ld, cols, buffer(in_stage, j), t);
+        if (j < in.left) fetch_row<XT, V, NV, TPR, LEAST>(x + (int64_t)(in.r + j) * a.x_ld, cols, buffer(in_stage, j), t);
       --to_fetch;
       advance(in);
       if (++in_stage == D) in_stage = 0;
@@ -71,7 +72,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
 #pragma unroll
     for (int j = 0; j < RB; ++j) odd[j] = j < w.left ? load_odd(x + (int64_t)(w.r + j) * a.x_ld, cols, t) : (uint16_t)0;
   };
-  auto here = [&](int i) { return FULL || (t + i * TPR) * V < cols; };
+  auto here = [&](int i) { return (i + 1) * TPR * V <= LEAST || (t + i * TPR) * V < cols; };
 
   Turn turn = begin_sums<CL>(sh);
   pdl_wait();
@@ -217,10 +218,10 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
   if (CL > 1) cluster_sync_all();                           // no block ends while another may write to its sums
 }
 
-template <typename XT, typename YT, int V, int NV, int TPR, int RB, int D, int CL, bool FULL>
+template <typename XT, typename YT, int V, int NV, int TPR, int RB, int D, int CL, int LEAST>
 cudaError_t launch(const NormForward& a, cudaStream_t stream) {
   constexpr int kThreads = TPR > kNormThreads ? TPR : kNormThreads, kSlots = kThreads / TPR;
-  const auto kernel = norm_forward_kernel<XT, YT, V, NV, TPR, RB, D, CL, FULL>;
+  const auto kernel = norm_forward_kernel<XT, YT, V, NV, TPR, RB, D, CL, LEAST>;
   // the most that any width of this instance asks for, and how many blocks an SM holds then
   constexpr int kMost = D * kSlots * RB * row_room(TPR * V * NV, sizeof(XT), V == 1);
   static_assert(kMost <= 225 * 1024, "ring too large");
@@ -245,34 +246,35 @@ bool dispatch(const NormForward& a, cudaStream_t stream, cudaError_t* e) {
   auto fits = [&](const void* p, int64_t ld, int size) { return (((uintptr_t)p | (uintptr_t)(ld * size)) & (V * size - 1)) == 0; };
   const bool pieces = a.cols % V == 0 && fits(a.x, a.x_ld, sizeof(XT)) && fits(a.y, a.y_ld, sizeof(YT));
   const int n = a.cols;
-#define TAKE(v, nv, tpr, rb, d, cl)                                                                  \
-  if ((v) > 1 && n == (v) * (nv) * (tpr) * (cl))                                                     \
-    return *e = launch<XT, YT, v, nv, tpr, rb, d, cl, (v > 1)>(a, stream), true;                     \
-  if (n <= (v) * (nv) * (tpr) * (cl)) return *e = launch<XT, YT, v, nv, tpr, rb, d, cl, false>(a, stream), true
+  // least: columns that are too many for the line before; of a cluster's block, which may have as little as none, 0
+#define TAKE(least, v, nv, tpr, rb, d, cl)                                                                  \
+  if ((v) > 1 && n == (v) * (nv) * (tpr) * (cl))                                                           \
+    return *e = launch<XT, YT, v, nv, tpr, rb, d, cl, (v) * (nv) * (tpr)>(a, stream), true;               \
+  if (n <= (v) * (nv) * (tpr) * (cl)) return *e = launch<XT, YT, v, nv, tpr, rb, d, cl, least>(a, stream), true
   if (pieces) {
-    TAKE(V, 1, 64 / V, 4, 3, 1);
-    TAKE(V, 1, 128 / V, 4, 3, 1);
-    TAKE(V, 8 / V, 32, 4, 3, 1);
-    TAKE(V, 16 / V, 32, 2, 3, 1);
-    TAKE(V, 16 / V, 64, 2, 3, 1);
-    TAKE(V, 16 / V, 128, 2, 3, 1);
-    TAKE(V, 16 / V, 256, 2, 3, 1);
-    TAKE(V, 16 / V, 512, 2, 2, 1);
-    TAKE(V, 32 / V, 512, 1, 3, 1);
-    TAKE(V, 32 / V, 512, 1, 3, 2);
-    TAKE(V, 32 / V, 512, 1, 3, 4);
+    TAKE(0, V, 1, 64 / V, 4, 3, 1);
+    TAKE(65, V, 1, 128 / V, 4, 3, 1);
+    TAKE(129, V, 8 / V, 32, 4, 3, 1);
+    TAKE(257, V, 16 / V, 32, 2, 3, 1);
+    TAKE(513, V, 16 / V, 64, 2, 3, 1);
+    TAKE(1025, V, 16 / V, 128, 2, 3, 1);
+    TAKE(2049, V, 16 / V, 256, 2, 3, 1);
+    TAKE(4097, V, 16 / V, 512, 2, 2, 1);
+    TAKE(8193, V, 32 / V, 512, 1, 3, 1);
+    TAKE(0, V, 32 / V, 512, 1, 3, 2);
+    TAKE(0, V, 32 / V, 512, 1, 3, 4);
   } else {
-    TAKE(1, 2, 8, 4, 3, 1);
-    TAKE(1, 2, 32, 4, 3, 1);
-    TAKE(1, 8, 32, 4, 3, 1);
-    TAKE(1, 16, 32, 2, 3, 1);
-    TAKE(1, 16, 64, 2, 3, 1);
-    TAKE(1, 16, 128, 2, 3, 1);
-    TAKE(1, 16, 256, 2, 3, 1);
-    TAKE(1, 16, 512, 2, 2, 1);
-    TAKE(1, 32, 512, 1, 3, 1);
-    TAKE(1, 32, 512, 1, 3, 2);
-    TAKE(1, 32, 512, 1, 3, 4);
+    TAKE(0, 1, 2, 8, 4, 3, 1);
+    TAKE(17, 1, 2, 32, 4, 3, 1);
+    TAKE(65, 1, 8, 32, 4, 3, 1);
+    TAKE(257, 1, 16, 32, 2, 3, 1);
+    TAKE(513, 1, 16, 64, 2, 3, 1);
+    TAKE(1025, 1, 16, 128, 2, 3, 1);
+    TAKE(2049, 1, 16, 256, 2, 3, 1);
+    TAKE(4097, 1, 16, 512, 2, 2, 1);
+    TAKE(8193, 1, 32, 512, 1, 3, 1);
+    TAKE(0, 1, 32, 512, 1, 3, 2);
+    TAKE(0, 1, 32, 512, 1, 3, 4);
   }
 #undef TAKE
   return false;

@@ -143,45 +143,50 @@ __host__ __device__ __forceinline__ constexpr int row_room(int cols, int size, b
   return (cols * size + (anywhere ? 15 : 0) + 127) / 128 * 128;
 }
 
-// Starts the copies of a row into `buf`.  FULL: the row has TPR * NV pieces.
-template <typename T, int V, int NV, int TPR, bool FULL>
+// Starts the copies of a row into `buf`.  LEAST: columns that it has at least.
+template <typename T, int V, int NV, int TPR, int LEAST>
 __device__ __forceinline__ void fetch_row(const T* row, int cols, char* buf, int t) {
   if (V > 1) {
     const T* const from = row + t * V;
     const uint32_t to = smem_u32(buf) + t * (V * sizeof(T));
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-      if (FULL || (t + i * TPR) * V < cols) copy_async<V * sizeof(T)>(to + i * (TPR * V * sizeof(T)), from + i * (TPR * V));
+      if ((i + 1) * TPR * V <= LEAST || (t + i * TPR) * V < cols) copy_async<V * sizeof(T)>(to + i * (TPR * V * sizeof(T)), from + i * (TPR * V));
   } else {
-    const uintptr_t first = (uintptr_t)row, last = first + (uintptr_t)cols * sizeof(T);
-    const uintptr_t base = first & ~(uintptr_t)15, whole = (first + 15) & ~(uintptr_t)15, end = last & ~(uintptr_t)15;
-    for (uintptr_t p = whole + 16 * t; p + 16 <= end; p += 16 * TPR)
-      copy_async<16>(smem_u32(buf + (p - base)), reinterpret_cast<const void*>(p));
-    // the ends, in fp32 words; single bf16 elements among them are left to fetch_odd
-    const uintptr_t head = whole < last ? whole : last;          // a short row may lie between two boundaries
-    const uintptr_t word = (first + 3) & ~(uintptr_t)3;
-    for (uintptr_t p = word + 4 * t; p + 4 <= head; p += 4 * TPR)
-      copy_async<4>(smem_u32(buf + (p - base)), reinterpret_cast<const void*>(p));
-    if (end >= whole)
-      for (uintptr_t p = end + 4 * t; p + 4 <= last; p += 4 * TPR)
-        copy_async<4>(smem_u32(buf + (p - base)), reinterpret_cast<const void*>(p));
+    // from the 16-byte boundary at or before the row: whole 16-byte pieces, then up to three fp32 words at either end; single
+    // bf16 elements outside these are left to load_odd
+    constexpr int kPieces = (TPR * NV * (int)sizeof(T) / 16 + TPR) / TPR;
+    const int off = (int)((uintptr_t)row & 15), end = off + cols * (int)sizeof(T);
+    const char* const base = reinterpret_cast<const char*>(row) - off;
+    const uint32_t to = smem_u32(buf);
+    const int head = (off + 15) >> 4, tail = end >> 4;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int p = head + t + i * TPR;
+      if (p < tail) copy_async<16>(to + p * 16, base + p * 16);
+    }
+    if (t < 8) {
+      const int p = t < 4 ? ((off + 3) >> 2) + t : tail * 4 + t - 4, past = t < 4 ? min(head * 4, end >> 2) : tail < head ? 0 : end >> 2;
+      if (p < past) copy_async<4>(to + p * 4, base + p * 4);
+    }
   }
 }
 // bf16 rows that start or end in the middle of a 4-byte word: thread 0 and thread 1 of the row carry those elements.
 template <typename T>
 __device__ __forceinline__ uint16_t load_odd(const T* row, int cols, int t) {
   if (sizeof(T) == 4) return 0;
-  const uintptr_t first = (uintptr_t)row, last = first + (uintptr_t)cols * sizeof(T);
-  if (t == 0 && (first & 3)) return *reinterpret_cast<const uint16_t*>(row);
-  if (t == 1 && (last & 3)) return *reinterpret_cast<const uint16_t*>(row + cols - 1);
-  return 0;
+  const int off = (int)((uintptr_t)row & 3) >> 1;
+  const int at = t == 0 ? 0 : cols - 1;
+  const bool mine = t == 0 ? off : t == 1 && ((off + cols) & 1);
+  return mine ? *reinterpret_cast<const uint16_t*>(row + at) : (uint16_t)0;
 }
 template <typename T>
 __device__ __forceinline__ void store_odd(const T* row, int cols, char* buf, int t, uint16_t v) {
   if (sizeof(T) == 4) return;
-  const uintptr_t first = (uintptr_t)row, last = first + (uintptr_t)cols * sizeof(T), base = first & ~(uintptr_t)15;
-  if (t == 0 && (first & 3)) *reinterpret_cast<uint16_t*>(buf + (first - base)) = v;
-  if (t == 1 && (last & 3)) *reinterpret_cast<uint16_t*>(buf + (last - 2 - base)) = v;
+  const int off = (int)((uintptr_t)row & 15) >> 1;
+  const int at = t == 0 ? 0 : cols - 1;
+  const bool mine = t == 0 ? off & 1 : t == 1 && ((off + cols) & 1);
+  if (mine) reinterpret_cast<uint16_t*>(buf)[off + at] = v;
 }
 
 typedef unsigned long long pair;        // two fp32 values
@@ -306,25 +311,30 @@ __device__ __forceinline__ void end_row_sums(float* v, S& sh, Turn* turn) {
     turn->parity ^= turn->buffer;          // the barrier's next use has the other parity
   }
   turn->buffer ^= 1;
+  if (W < 8) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if (W <= 8) {
+    for (int i = 0; i < N; ++i) {
       float s = b[i * W];
 #pragma unroll
       for (int w = 1; w < W; ++w) s += b[i * W + w];
       v[i] = s;
-    } else {
-      float s = lane < W ? b[i * W + lane] : 0.f;
-#pragma unroll
-      for (int w = 32; w < W; w += 32) s += b[i * W + w + lane];
-#pragma unroll
-      for (int o = (W < 32 ? W : 32) / 2; o; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
-      v[i] = W < 32 ? __shfl_sync(0xffffffffu, s, 0) : s;
     }
-    if (CL > 1 && turn->gave_up) v[i] = __uint_as_float(0x7fc00000u);
+  } else {
+    // a part of the warp's lanes for each value
+    constexpr int G = 32 / N;
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; w += G)
+      if (W >= G || lane % G < W) s += b[lane / G * W + w + lane % G];
+#pragma unroll
+    for (int o = G / 2; o; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, s, i * G);
   }
+  if (CL > 1 && turn->gave_up)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __uint_as_float(0x7fc00000u);
 }
-
 template <int TPR, int CL, int N, typename S>
 __device__ __forceinline__ void row_sums(float* v, S& sh, Turn* turn) {
   begin_row_sums<TPR, CL, N>(v, sh, *turn);
