@@ -7,9 +7,9 @@
 #include <type_traits>
 
 #include "kernels.h"
+#include "pairs.cuh"
 
-using namespace ist;
-
+namespace ist {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
@@ -155,39 +155,31 @@ __device__ __forceinline__ void put_codes(uint8_t* p, int64_t i, int64_t n, bool
   }
 }
 
-__device__ __forceinline__ void put8(float* p, int64_t i, int64_t n, bool vec, const float v[8]) {
-  put4(p, i, n, vec, v);
-  put4(p, i + 4, n, vec, v + 4);
-}
-__device__ __forceinline__ void put8(bf16* p, int64_t i, int64_t n, bool vec, const float v[8]) {
-  if (vec && i + 8 <= n) {
-    uint4 o;
-    uint32_t* const w = reinterpret_cast<uint32_t*>(&o);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-      w[k] = *reinterpret_cast<const uint32_t*>(&b);
-    }
-    *reinterpret_cast<uint4*>(p + i) = o;
-  } else {
-    put4(p, i, n, false, v);
-    put4(p, i + 4, n, false, v + 4);
-  }
-}
-
 // The moments' products and sums are rounded one by one, as elementary operations would be: 8-bit codes hang on their bits.
 __device__ __forceinline__ void moments(const Args& a, float clip, float g, float* m, float* v) {
   g = __fmul_rn(g, clip);
   *m = __fadd_rn(__fmul_rn(a.b1, *m), __fmul_rn(a.c1, g));
   *v = __fadd_rn(__fmul_rn(a.b2, *v), __fmul_rn(__fmul_rn(a.c2, g), g));
 }
-// The root and the quotient by the hardware's approximations (2^-23 and 2^-22 of their values at most; the divisor is a normal
-// number, eps at least): the change of a parameter is exact to a few units in its last place, and in the 8-bit step instructions
-// are what the time goes to.
+// The root and the reciprocal by the hardware's approximations (2^-23 of their values each; the divisor is a normal number, eps
+// at least, and far from the largest): the change of a parameter is exact to a few units in its last place, and in the
+// 8-bit step instructions are what the time goes to.  TINY: eps is so small that roots of denormal numbers weigh beside it.
+template <bool TINY>
+__device__ __forceinline__ float root_of(float v) {
+  float r;
+  if (TINY)
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+  else
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float inverse(float a) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(a));
+  return r;
+}
 __device__ __forceinline__ float update(const Args& a, const Step& s, float decay, float p, float m, float v) {
-  float root;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v));
-  return fmaf(-s.step_size, __fdividef(m, fmaf(root, s.inv_root, a.eps)), fmaf(-s.lr * decay, p, p));
+  return fmaf(-s.step_size, m * inverse(fmaf(root_of<true>(v), s.inv_root, a.eps)), fmaf(-s.lr * decay, p, p));
 }
 
 template <typename GT, int CAP>
@@ -224,47 +216,71 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
   }
 }
 
-// Four codes of a block become values; see ist.h.  CHECKED: a base that no step makes reads as an infinity where it leaves
-// fp32 (without it, as whatever number the sum's bits are).  The largest code is looked for in all four at once.
-template <bool CHECKED>
+// Four codes of a block become values; see ist.h.  Bases that no step makes read as infinities where they leave fp32.  TOP: the
+// largest code, 127 or 255.  Not inlined: what seldom runs would otherwise be issued, predicated off, with what always does.
+template <uint32_t TOP>
+__device__ __noinline__ float4 decode_any4(uint32_t w, int base) {
+  float x[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t one = w >> (8 * k) & 255u, c = one & TOP;
+    uint32_t bits = c == TOP ? (TOP == 127u ? 0x7fc00000u : kInfinity) : min((uint32_t)base + c, kInfinity >> 20) << 20;
+    if (c == 0) bits = 0;
+    x[k] = __uint_as_float(bits | (one & ~TOP) << 24);
+  }
+  return make_float4(x[0], x[1], x[2], x[3]);
+}
+// The same for bases that steps make: a code is multiplied into its place and the base is added, unless one of the four is zero or
+// the largest.
 __device__ __forceinline__ void decode_m4(uint32_t w, int base, float* m) {
+  const uint32_t c = w & 0x7f7f7f7fu, sign = w & 0x80808080u, b = (uint32_t)base << 20;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint32_t c = (k == 3 ? w >> 4 : w << (20 - 8 * k)) & 0x07f00000u;
-    uint32_t bits = CHECKED ? min((uint32_t)base + (c >> 20), kInfinity >> 20) << 20 : ((uint32_t)base << 20) + c;
-    if (c == 0) bits = 0;
-    m[k] = __uint_as_float(bits | ((w << (24 - 8 * k)) & 0x80000000u));
+  for (int k = 0; k < 4; ++k)
+    m[k] = __uint_as_float((__byte_perm(c, 0, 0x4440 + k) * (1u << 20) + b) | __byte_perm(sign, 0, 0x0444 + (k << 12)));
+  if (((c + 0x01010101u) | ~(c + 0x7f7f7f7fu)) & 0x80808080u) {
+    const float4 f = decode_any4<127>(w, base);
+    m[0] = f.x; m[1] = f.y; m[2] = f.z; m[3] = f.w;
   }
-  if (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u)
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (((w >> (8 * k)) & 127u) == 127u) m[k] = __uint_as_float(0x7fc00000u);
 }
-template <bool CHECKED>
 __device__ __forceinline__ void decode_v4(uint32_t w, int base, float* v) {
+  const uint32_t b = (uint32_t)base << 20;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint32_t c = (k == 3 ? w >> 4 : w << (20 - 8 * k)) & 0x0ff00000u;
-    uint32_t bits = CHECKED ? min((uint32_t)base + (c >> 20), kInfinity >> 20) << 20 : ((uint32_t)base << 20) + c;
-    if (c == 0) bits = 0;
-    v[k] = __uint_as_float(bits);
+  for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(__byte_perm(w, 0, 0x4440 + k) * (1u << 20) + b);
+  if ((((w - 0x01010101u) & ~w) | ((~w - 0x01010101u) & w)) & 0x80808080u) {
+    const float4 f = decode_any4<255>(w, base);
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
   }
-  if ((~w - 0x01010101u) & w & 0x80808080u)              // a byte of ~w is zero
+}
+// The top bytes of four words.
+__device__ __forceinline__ uint32_t top4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
+
+// Codes of four values, bits of their magnitudes and their noise given, where one of the block's is not finite or near fp32's largest.
+__device__ __noinline__ uint32_t encode_special4(uint4 bits, uint4 noise, int base, uint32_t top) {
+  const uint32_t b[4] = {bits.x, bits.y, bits.z, bits.w}, r[4] = {noise.x, noise.y, noise.z, noise.w};
+  uint32_t w = 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (((w >> (8 * k)) & 255u) == 255u) v[k] = __uint_as_float(kInfinity);
+  for (int k = 0; k < 4; ++k)
+    w |= (b[k] >= kInfinity ? top : (uint32_t)max((int)min((b[k] + r[k] * 16u + 8u) >> 20, kLargest) - base, 0)) << (8 * k);
+  return w;
 }
-template <int BYTES>
-__device__ __forceinline__ void copy_async(void* to, const void* from) {
-  const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
-  if (BYTES == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(BYTES) : "memory");
+// Zero codes of values that are not zero become the smallest code.
+__device__ __noinline__ uint32_t lift_zeros4(uint32_t codes, uint4 bits) {
+  const uint32_t b[4] = {bits.x, bits.y, bits.z, bits.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (b[k] && !(codes >> (8 * k) & 255u)) codes |= 1u << (8 * k);
+  return codes;
 }
-// Four bytes, one of each word's lowest.
-__device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+// Largest of the bits that belong to numbers.
+__device__ __noinline__ uint32_t largest_number(uint4 bits) {
+  const uint32_t b[4] = {bits.x, bits.y, bits.z, bits.w};
+  uint32_t m = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (b[k] < kInfinity) m = max(m, b[k]);
+  return m;
 }
 
 // A warp takes 128 values that share a base, four to a lane; a block takes a chunk, each of its warps t.per blocks of 128 in a
@@ -274,42 +290,59 @@ __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, ui
 // and none near fp32's largest, which is to say all of a healthy run's, take a path without the cases of the others.
 constexpr int kMostPer = 16, kStages = 4;
 
-template <typename GT, int CAP>
-__global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant__ Table<CAP> t, const Args a) {
-  pdl_wait();
-  pdl_trigger();
-  const Step s = begin_step(a);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+template <bool TINY, typename GT, int CAP>
+__device__ __forceinline__ void adamw8_chunks(const Table<CAP>& t, const Args& a, const Step& s, char* ring) {
   constexpr int kStage = kBlock * (4 + sizeof(GT) + 2);      // a block's p, g and codes
-  extern __shared__ __align__(128) char rings[];
-  char* const ring = rings + warp * (kStages * kStage);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const pair b1 = both(a.b1), c1 = both(a.c1), b2 = both(a.b2), c2 = both(a.c2), clip = both(s.clip);
+  const pair inv_root = both(s.inv_root), eps = both(a.eps), step = both(-s.step_size);
   for (int c = blockIdx.x; c < t.chunk0[t.count]; c += gridDim.x) {
     const int j = find_tensor(t, c);
     const Entry& e = t.e[j];
-    // from the warp's first value on
-    const int64_t first = ((int64_t)(c - t.chunk0[j]) * kWarps + warp) * (t.per * kBlock), left = e.n - first;
+    // the chunk's first value (the same for all threads), and where in the chunk this lane's first one is
+    const int64_t first = (int64_t)(c - t.chunk0[j]) * (kWarps * t.per * kBlock);
+    const uint32_t mine = warp * (t.per * kBlock) + lane * 4;
+    const int64_t left = e.n - first - warp * (t.per * kBlock);
     if (left <= 0) continue;
     float* const p = e.p + first;
     const GT* const g = (const GT*)e.g + first;
     uint8_t* const m = (uint8_t*)e.m + first;
     uint8_t* const v = (uint8_t*)e.v + first;
     bf16* const copy = e.copy ? e.copy + first : nullptr;
-    int16_t* const mb = e.mb + first / kBlock;
-    int16_t* const vb = e.vb + first / kBlock;
-    const float decay = e.decay;
+    const pair decay = both(-s.lr * e.decay);
+    const int blocks = (int)min((int64_t)t.per, ceil_div(left, kBlock));
+    const int whole = e.index & kAligned ? (int)min((int64_t)t.per, left / kBlock) : 0;
     // word w of the noise belongs to values 2 w and 2 w + 1
-    const uint64_t noise = splitmix64(s.key, (e.index & ~kAligned) + 1ull) + kGolden * (uint64_t)(first / 2 + lane * 2 + 1);
-    auto work = [&](auto fast, int u, float (&pf)[4], const float (&gf)[4], uint32_t mc, uint32_t vc, int mbase, int vbase) {
+    uint64_t noise = splitmix64(s.key, (e.index & ~kAligned) + 1ull) + kGolden * (uint64_t)((first + mine) / 2 + 1);
+    // lane u has the first moment's base of block u, lane 16 + u the second's
+    int16_t* const my_base = (lane < 16 ? e.mb : e.vb) + first / kBlock + warp * t.per + (lane & 15);
+    const int base = (lane & 15) < blocks ? *my_base : 0;
+    int new_base = 0;
+
+    auto work = [&](int u, float (&pf)[4], const float (&gf)[4], uint32_t mc, uint32_t vc, uint32_t* mw, uint32_t* vw) {
       float mf[4], vf[4];
-      decode_m4<false>(mc, mbase, mf);
-      decode_v4<false>(vc, vbase, vf);
+      decode_m4(mc, __shfl_sync(0xffffffffu, base, u), mf);
+      decode_v4(vc, __shfl_sync(0xffffffffu, base, 16 + u), vf);
       uint32_t mbits[4], vbits[4], mmax = 0, vmax = 0;
+      // the moments: the same operations, one rounding each, as in moments()
+#pragma unroll
+      for (int k = 0; k < 4; k += 2) {
+        const pair gc = mul(make_pair2(gf[k], gf[k + 1]), clip);
+        const pair mn = add(mul(b1, make_pair2(mf[k], mf[k + 1])), mul(c1, gc));
+        const pair vn = add(mul(b2, make_pair2(vf[k], vf[k + 1])), mul(mul(c2, gc), gc));
+        const pair d = fma(make_pair2(root_of<TINY>(first_of(vn)), root_of<TINY>(second_of(vn))), inv_root, eps);
+        const pair q = mul(mn, make_pair2(inverse(first_of(d)), inverse(second_of(d))));
+        const pair po = make_pair2(pf[k], pf[k + 1]), pn = fma(step, q, fma(decay, po, po));
+        pf[k] = first_of(pn);
+        pf[k + 1] = second_of(pn);
+        mf[k] = first_of(mn);
+        mf[k + 1] = second_of(mn);
+        vbits[k] = __float_as_uint(first_of(vn));                  // of a number: the sign is zero
+        vbits[k + 1] = __float_as_uint(second_of(vn));
+      }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        moments(a, s.clip, gf[k], &mf[k], &vf[k]);
-        pf[k] = update(a, s, decay, pf[k], mf[k], vf[k]);
         mbits[k] = __float_as_uint(mf[k]) & 0x7fffffffu;
-        vbits[k] = __float_as_uint(vf[k]);                       // of a number: the sign is zero
         mmax = max(mmax, mbits[k]);
         vmax = max(vmax, vbits[k]);
       }
@@ -317,95 +350,103 @@ __global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant_
       vmax = __reduce_max_sync(0xffffffffu, vmax);
       const bool special = max(mmax, vmax) >= kLargest << 20;
       if (special) {
-        mmax = vmax = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          vbits[k] &= 0x7fffffffu;
-          if (mbits[k] < kInfinity) mmax = max(mmax, mbits[k]);
-          if (vbits[k] < kInfinity) vmax = max(vmax, vbits[k]);
-        }
-        mmax = __reduce_max_sync(0xffffffffu, mmax);
-        vmax = __reduce_max_sync(0xffffffffu, vmax);
+        for (int k = 0; k < 4; ++k) vbits[k] &= 0x7fffffffu;
+        mmax = __reduce_max_sync(0xffffffffu, largest_number(make_uint4(mbits[0], mbits[1], mbits[2], mbits[3])));
+        vmax = __reduce_max_sync(0xffffffffu, largest_number(make_uint4(vbits[0], vbits[1], vbits[2], vbits[3])));
       }
       // the block's largest value, rounded up, gets the largest code but one
       const int nmb = max((int)(mmax >> 20) + 1 - 126, 0), nvb = max((int)(vmax >> 20) + 1 - 254, 0);
-      const uint32_t mlow = 8u - ((uint32_t)nmb << 20), vlow = 8u - ((uint32_t)nvb << 20);
-      uint32_t cm[4], cv[4];
+      if ((lane & 15) == u) new_base = lane < 16 ? nmb : nvb;
+      const int mlow = 8 - (nmb << 20), vlow = 8 - (nvb << 20);
+      uint32_t mr[4], vr[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const uint64_t w = mix64(noise + kGolden * (uint64_t)(u * (kBlock / 2) + k / 2));
+        const uint64_t w = mix64(noise + kGolden * (uint64_t)(k / 2));
         const uint32_t r = k & 1 ? (uint32_t)(w >> 32) : (uint32_t)w;
-        const uint32_t mr = r << 4 & 0xffff0u, vr = r >> 12 & 0xffff0u;
-        if (!special) {
-          cm[k] = (uint32_t)max((int)(mbits[k] + mr + mlow), 0) >> 20;
-          cv[k] = (uint32_t)max((int)(vbits[k] + vr + vlow), 0) >> 20;
-        } else {
-          cm[k] = mbits[k] >= kInfinity ? 127u : (uint32_t)max((int)min((mbits[k] + mr + 8u) >> 20, kLargest) - nmb, 0);
-          cv[k] = vbits[k] >= kInfinity ? 255u : (uint32_t)max((int)min((vbits[k] + vr + 8u) >> 20, kLargest) - nvb, 0);
+        mr[k] = r & 0xffffu;
+        vr[k] = r >> 16;
+      }
+      noise += kGolden * (uint64_t)(kBlock / 2);
+      uint32_t codes, out;
+      if (!special) {
+        uint32_t cm[4], cv[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {                                     // the code is the top byte
+          cm[k] = (uint32_t)__viaddmax_s32((int)(mr[k] * 16u + mbits[k]), mlow, 0) * 16u;
+          cv[k] = (uint32_t)__viaddmax_s32((int)(vr[k] * 16u + vbits[k]), vlow, 0) * 16u;
         }
-        cv[k] = max(cv[k], min(vbits[k], 1u));                   // a divisor does not vanish
-        if (cm[k]) cm[k] |= (__float_as_uint(mf[k]) >> 24) & 128u;
-      }
-      const uint32_t mw = pack4(cm[0], cm[1], cm[2], cm[3]), vw = pack4(cv[0], cv[1], cv[2], cv[3]);
-      const int i = u * kBlock + lane * 4;
-      if (fast) {
-        store4(p + i, pf);
-        if (copy) store4(copy + i, pf);
-        *reinterpret_cast<uint32_t*>(m + i) = mw;
-        *reinterpret_cast<uint32_t*>(v + i) = vw;
+        codes = top4(cm[0], cm[1], cm[2], cm[3]);
+        out = top4(cv[0], cv[1], cv[2], cv[3]);
       } else {
-        const bool vec = e.index & kAligned;
-        put4(p, i, left, vec, pf);
-        if (copy) put4(copy, i, left, vec, pf);
-        put_codes(m, i, left, vec, mw);
-        put_codes(v, i, left, vec, vw);
+        codes = encode_special4(make_uint4(mbits[0], mbits[1], mbits[2], mbits[3]), make_uint4(mr[0], mr[1], mr[2], mr[3]), nmb, 127u);
+        out = encode_special4(make_uint4(vbits[0], vbits[1], vbits[2], vbits[3]), make_uint4(vr[0], vr[1], vr[2], vr[3]), nvb, 255u);
       }
-      if (lane == 0) {
-        mb[u] = (int16_t)nmb;
-        vb[u] = (int16_t)nvb;
-      }
+      const uint32_t signs = top4(__float_as_uint(mf[0]), __float_as_uint(mf[1]), __float_as_uint(mf[2]), __float_as_uint(mf[3]));
+      *mw = codes | (signs & (codes + 0x7f7f7f7fu) & 0x80808080u);      // a zero has no sign
+      if ((out - 0x01010101u) & ~out & 0x80808080u)                     // a divisor does not vanish
+        out = lift_zeros4(out, make_uint4(vbits[0], vbits[1], vbits[2], vbits[3]));
+      *vw = out;
     };
-    const int blocks = (int)min((int64_t)t.per, ceil_div(left, kBlock));
-    const int whole = e.index & kAligned ? (int)min((int64_t)t.per, left / kBlock) : 0;
     auto fetch = [&](int u) {
       if (u < whole) {
         char* const to = ring + (u % kStages) * kStage;
-        const int i = u * kBlock + lane * 4;
-        copy_async<16>(to + lane * 16, p + i);
-        copy_async<4 * sizeof(GT)>(to + kBlock * 4 + lane * (4 * sizeof(GT)), g + i);
-        copy_async<4>(to + kBlock * (4 + sizeof(GT)) + lane * 4, m + i);
-        copy_async<4>(to + kBlock * (5 + sizeof(GT)) + lane * 4, v + i);
+        const uint32_t i = mine + u * kBlock;
+        copy_async<16>(shared_address(to + lane * 16), p + i);
+        copy_async<4 * sizeof(GT)>(shared_address(to + kBlock * 4 + lane * (4 * sizeof(GT))), g + i);
+        copy_async<4>(shared_address(to + kBlock * (4 + sizeof(GT)) + lane * 4), m + i);
+        copy_async<4>(shared_address(to + kBlock * (5 + sizeof(GT)) + lane * 4), v + i);
       }
-      asm volatile("cp.async.commit_group;" ::: "memory");
+      copy_commit();
     };
 #pragma unroll
     for (int u = 0; u < kStages - 1; ++u) fetch(u);
-    // lane u has the first moment's base of block u, lane 16 + u the second's
-    const int base = (lane & 15) < blocks ? (lane < 16 ? mb : vb)[lane & 15] : 0;
 #pragma unroll 1
     for (int u = 0; u < whole; ++u) {
       fetch(u + kStages - 1);
-      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+      copy_wait<kStages - 1>();
       const char* const from = ring + (u % kStages) * kStage;
       float pf[4], gf[4];
       load4(reinterpret_cast<const float*>(from) + lane * 4, pf);
       load4(reinterpret_cast<const GT*>(from + kBlock * 4) + lane * 4, gf);
-      const uint32_t mc = reinterpret_cast<const uint32_t*>(from + kBlock * (4 + sizeof(GT)))[lane];
-      const uint32_t vc = reinterpret_cast<const uint32_t*>(from + kBlock * (5 + sizeof(GT)))[lane];
-      work(std::true_type(), u, pf, gf, mc, vc, __shfl_sync(0xffffffffu, base, u), __shfl_sync(0xffffffffu, base, 16 + u));
+      uint32_t mw = reinterpret_cast<const uint32_t*>(from + kBlock * (4 + sizeof(GT)))[lane];
+      uint32_t vw = reinterpret_cast<const uint32_t*>(from + kBlock * (5 + sizeof(GT)))[lane];
+      work(u, pf, gf, mw, vw, &mw, &vw);
+      const uint32_t i = mine + u * kBlock;
+      store4(p + i, pf);
+      if (copy) store4(copy + i, pf);
+      *reinterpret_cast<uint32_t*>(m + i) = mw;
+      *reinterpret_cast<uint32_t*>(v + i) = vw;
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    copy_wait<0>();
 #pragma unroll 1
     for (int u = whole; u < blocks; ++u) {
       const bool vec = e.index & kAligned;
-      const int i = u * kBlock + lane * 4;
+      const int64_t i = mine + u * kBlock, n = e.n - first;
       float pf[4], gf[4];
-      get4(p, i, left, vec, pf);
-      get4(g, i, left, vec, gf);
-      work(std::false_type(), u, pf, gf, get_codes(m, i, left, vec), get_codes(v, i, left, vec), __shfl_sync(0xffffffffu, base, u),
-           __shfl_sync(0xffffffffu, base, 16 + u));
+      get4(p, i, n, vec, pf);
+      get4(g, i, n, vec, gf);
+      uint32_t mw, vw;
+      work(u, pf, gf, get_codes(m, i, n, vec), get_codes(v, i, n, vec), &mw, &vw);
+      put4(p, i, n, vec, pf);
+      if (copy) put4(copy, i, n, vec, pf);
+      put_codes(m, i, n, vec, mw);
+      put_codes(v, i, n, vec, vw);
     }
+    if ((lane & 15) < blocks) *my_base = (int16_t)new_base;
   }
+}
+
+template <typename GT, int CAP>
+__global__ void __launch_bounds__(kThreads, 3) adamw8_kernel(const __grid_constant__ Table<CAP> t, const Args a) {
+  extern __shared__ __align__(128) char rings[];
+  char* const ring = rings + (threadIdx.x >> 5) * (kStages * kBlock * (4 + sizeof(GT) + 2));
+  pdl_wait();
+  pdl_trigger();
+  const Step s = begin_step(a);
+  // roots of denormal numbers are below 2^-63: beside a divisor of 2^-36 and more they do not show
+  if (a.eps >= 0x1p-36f && s.inv_root <= 0x1p3f) adamw8_chunks<false, GT>(t, a, s, ring);
+  else adamw8_chunks<true, GT>(t, a, s, ring);
 }
 
 // Sum of squares of all gradients, a partial sum per block.  Eight squares at a time are added in fp32 and
@@ -445,38 +486,80 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_consta
   if (threadIdx.x == 0) partials[blockIdx.x] = sum;
 }
 
-// Eight values to a thread where a state's arrays allow it.
+template <typename OT>
+__device__ __forceinline__ void write8(OT* out, const float* x) {
+  if constexpr (sizeof(OT) == 2) {
+    uint4 o;
+    uint32_t* const w = reinterpret_cast<uint32_t*>(&o);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]);
+      w[k] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    *reinterpret_cast<uint4*>(out) = o;
+  } else {
+    store4(out, x);
+    store4(out + 4, x + 4);
+  }
+}
+template <bool SIGNED>
+__device__ __forceinline__ void decode4(uint32_t w, int base, float* x) {
+  constexpr uint32_t kTop = SIGNED ? 127u : 255u;
+  if ((uint32_t)base > kLargest - kTop) {
+    const float4 f = decode_any4<kTop>(w, base);
+    x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
+  } else if (SIGNED) {
+    decode_m4(w, base, x);
+  } else {
+    decode_v4(w, base, x);
+  }
+}
+// The values of one state.  Where its arrays allow it, eight to a thread; four loads and the bases of a thread's runs are on
+// their way together.
+template <bool SIGNED, typename OT>
+__device__ __forceinline__ void state_values(const uint8_t* codes, const int16_t* bases, int64_t n, bool vec, OT* out) {
+  constexpr int U = 4;
+  const int64_t step = (int64_t)gridDim.x * kThreads * 8;
+  int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 8;
+  for (; vec && i + (U - 1) * step + 8 <= n; i += U * step) {
+    uint2 c[U];
+    int base[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      c[u] = *reinterpret_cast<const uint2*>(codes + i + u * step);
+      base[u] = bases[(uint64_t)(i + u * step) / kBlock];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float x[8];
+      decode4<SIGNED>(c[u].x, base[u], x);
+      decode4<SIGNED>(c[u].y, base[u], x + 4);
+      write8(out + i + u * step, x);
+    }
+  }
+  for (; vec && i + 8 <= n; i += step) {
+    const uint2 c = *reinterpret_cast<const uint2*>(codes + i);
+    const int base = bases[(uint64_t)i / kBlock];
+    float x[8];
+    decode4<SIGNED>(c.x, base, x);
+    decode4<SIGNED>(c.y, base, x + 4);
+    write8(out + i, x);
+  }
+  for (; i < n; i += step)
+#pragma unroll 1
+    for (int h = 0; h < 8 && i + h < n; h += 4) {
+      float x[4];
+      decode4<SIGNED>(get_codes(codes, i + h, n, false), bases[(uint64_t)i / kBlock], x);
+      put4(out, i + h, n, false, x);
+    }
+}
 template <typename OT>
 __global__ void __launch_bounds__(kThreads) state_values_kernel(const uint8_t* m, const int16_t* mb, const uint8_t* v,
                                                                const int16_t* vb, int64_t n, bool vec, OT* m_out, OT* v_out) {
   pdl_wait();
   pdl_trigger();
-  const int64_t step = (int64_t)gridDim.x * kThreads * 8;
-  for (int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 8; i < n; i += step) {
-    uint32_t mc[2], vc[2];
-    int mbase = 0, vbase = 0;
-    if (m_out) {
-      mbase = mb[i / kBlock];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) mc[h] = get_codes(m, i + 4 * h, n, vec);
-    }
-    if (v_out) {
-      vbase = vb[i / kBlock];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) vc[h] = get_codes(v, i + 4 * h, n, vec);
-    }
-    float x[8];
-    if (m_out) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) decode_m4<true>(mc[h], mbase, x + 4 * h);
-      put8(m_out, i, n, vec, x);
-    }
-    if (v_out) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) decode_v4<true>(vc[h], vbase, x + 4 * h);
-      put8(v_out, i, n, vec, x);
-    }
-  }
+  if (m_out) state_values<true>(m, mb, n, vec, m_out);
+  if (v_out) state_values<false>(v, vb, n, vec, v_out);
 }
 
 bool aligned(const void* p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
@@ -588,6 +671,9 @@ const char* bad_tensor(const ist_adamw_tensor& x, const ist_adamw_args& a) {
 }
 
 }  // namespace
+}  // namespace ist
+
+using namespace ist;
 
 extern "C" size_t ist_adamw_workspace_bytes(int64_t count) {
   if (count < 0 || count > (int64_t)1 << 24) return 0;
@@ -658,8 +744,8 @@ extern "C" ist_status ist_adamw_state_values(const uint8_t* exp_avg, const int16
   if (why) return fail_call(IST_ERR_ARG, "ist_adamw_state_values: %s", why);
   if (n == 0 || (!exp_avg_out_dev && !exp_avg_sq_out_dev)) return IST_OK;
   cudaStream_t stream = (cudaStream_t)cuda_stream;
-  const bool vec = (!exp_avg_out_dev || (aligned(exp_avg, 4) && aligned(exp_avg_out_dev, 16))) &&
-                   (!exp_avg_sq_out_dev || (aligned(exp_avg_sq, 4) && aligned(exp_avg_sq_out_dev, 16)));
+  const bool vec = (!exp_avg_out_dev || (aligned(exp_avg, 8) && aligned(exp_avg_out_dev, 16))) &&
+                   (!exp_avg_sq_out_dev || (aligned(exp_avg_sq, 8) && aligned(exp_avg_sq_out_dev, 16)));
   const dim3 grid((unsigned)std::min<int64_t>(ceil_div(n, 8 * kThreads), (int64_t)sm_count() * 8));
   const cudaError_t e =
       out_type == IST_T_BF16

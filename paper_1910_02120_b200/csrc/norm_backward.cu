@@ -147,8 +147,8 @@ __global__ void __launch_bounds__(NV * V == 16 ? 512 : kNormThreads) norm_backwa
             s1 = fma(g, h, s1);
           }
         }
-        n[j] = first(s0) + second(s0);
-        n[RB + j] = first(s1) + second(s1);
+        n[j] = first_of(s0) + second_of(s0);
+        n[RB + j] = first_of(s1) + second_of(s1);
       }
       if (a.dx) begin_row_sums<TPR, CL, 2 * RB>(n, sh, turn);
     }
@@ -169,8 +169,8 @@ __global__ void __launch_bounds__(NV * V == 16 ? 512 : kNormThreads) norm_backwa
               const int q = i * V / 2 + e;
               const pair h = mul(add(make_pair2(xv[2 * e], xv[2 * e + 1]), minus), rs);
               const pair o = mul(fma(h, m1, fma(make_pair2(dv[2 * e], dv[2 * e + 1]), w[q], m0)), rs);
-              xv[2 * e] = first(o);
-              xv[2 * e + 1] = second(o);
+              xv[2 * e] = first_of(o);
+              xv[2 * e + 1] = second_of(o);
             }
 #pragma unroll
             for (int u = 0; u < kStep; ++u)
@@ -203,8 +203,8 @@ __global__ void __launch_bounds__(NV * V == 16 ? 512 : kNormThreads) norm_backwa
     float* const f = reinterpret_cast<float*>(ring);        // [slot][2][C][TPR]
 #pragma unroll
     for (int e = 0; e < C; ++e) {
-      f[((slot * 2 + 0) * C + e) * TPR + t] = e % 2 ? second(aw[e / 2]) : first(aw[e / 2]);
-      f[((slot * 2 + 1) * C + e) * TPR + t] = e % 2 ? second(ab[e / 2]) : first(ab[e / 2]);
+      f[((slot * 2 + 0) * C + e) * TPR + t] = e % 2 ? second_of(aw[e / 2]) : first_of(aw[e / 2]);
+      f[((slot * 2 + 1) * C + e) * TPR + t] = e % 2 ? second_of(ab[e / 2]) : first_of(ab[e / 2]);
     }
     __syncthreads();
     for (int q = threadIdx.x; q < 2 * C * TPR; q += kThreads) {
@@ -221,8 +221,8 @@ __global__ void __launch_bounds__(NV * V == 16 ? 512 : kNormThreads) norm_backwa
     for (int e = 0; e < C; ++e) {
       const int c = (t + e / V * TPR) * V + e % V;
       if (c < cols) {
-        if (a.wsum) a.wsum[at + c] = e % 2 ? second(aw[e / 2]) : first(aw[e / 2]);
-        if (a.bsum) a.bsum[at + c] = e % 2 ? second(ab[e / 2]) : first(ab[e / 2]);
+        if (a.wsum) a.wsum[at + c] = e % 2 ? second_of(aw[e / 2]) : first_of(aw[e / 2]);
+        if (a.bsum) a.bsum[at + c] = e % 2 ? second_of(ab[e / 2]) : first_of(ab[e / 2]);
       }
     }
   }

@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
         v[j][e] = make_pair2(f[2 * e], f[2 * e + 1]);
         sum = add(sum, v[j][e]);
       }
-      s[j] = first(sum) + second(sum);
+      s[j] = first_of(sum) + second_of(sum);
     }
     row_sums<TPR, CL, RB>(s, sh, &turn);
     float q[2 * RB];
@@ -147,14 +147,14 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
         pair d = add(v[j][e], minus);
         if (!FULL) {
           const bool one = here(2 * e / V), two = V == 1 ? here(2 * e + 1) : one;
-          d = make_pair2(one ? first(d) : 0.f, two ? second(d) : 0.f);
+          d = make_pair2(one ? first_of(d) : 0.f, two ? second_of(d) : 0.f);
         }
         v[j][e] = d;
         d1 = add(d1, d);
         d2 = fma(d, d, d2);
       }
-      q[j] = first(d1) + second(d1);
-      q[RB + j] = first(d2) + second(d2);
+      q[j] = first_of(d1) + second_of(d1);
+      q[RB + j] = first_of(d2) + second_of(d2);
     }
     row_sums<TPR, CL, 2 * RB>(q, sh, &turn);
     pair rstd[RB], shift[RB];
@@ -201,8 +201,8 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
           const pair r = fma(fma(v[j][p0 + e], rstd[j], shift[j]), wv[e], bv[e]);
-          o[2 * e] = first(r);
-          o[2 * e + 1] = second(r);
+          o[2 * e] = first_of(r);
+          o[2 * e + 1] = second_of(r);
         }
         if (j < now.left) {
           YT* const to = y + (int64_t)(now.r + j) * a.y_ld + t * V;

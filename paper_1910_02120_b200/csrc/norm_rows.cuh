@@ -12,6 +12,7 @@
 #pragma once
 
 #include "kernels.h"
+#include "pairs.cuh"
 #include "tc_ptx.cuh"
 
 namespace ist {
@@ -55,17 +56,6 @@ constexpr int kNormWidest = 65536;
 inline int norm_cluster(int64_t cols) { return cols <= 8192 ? 1 : cols <= 16384 ? 2 : cols <= 32768 ? 4 : 8; }
 
 namespace {
-
-template <int BYTES>
-__device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
-  if (BYTES == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // Writes to the place in block `rank` of the cluster that corresponds to `at` in this one; the write itself tells that block's
 // barrier, so no fence stands behind it (a cluster barrier would wait for all of the threads' stores to global memory too:
@@ -148,7 +138,7 @@ template <typename T, int V, int NV, int TPR, int LEAST>
 __device__ __forceinline__ void fetch_row(const T* row, int cols, char* buf, int t) {
   if (V > 1) {
     const T* const from = row + t * V;
-    const uint32_t to = smem_u32(buf) + t * (V * sizeof(T));
+    const uint32_t to = shared_address(buf) + t * (V * sizeof(T));
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if ((i + 1) * TPR * V <= LEAST || (t + i * TPR) * V < cols) copy_async<V * sizeof(T)>(to + i * (TPR * V * sizeof(T)), from + i * (TPR * V));
@@ -158,7 +148,7 @@ __device__ __forceinline__ void fetch_row(const T* row, int cols, char* buf, int
     constexpr int kPieces = (TPR * NV * (int)sizeof(T) / 16 + TPR) / TPR;
     const int off = (int)((uintptr_t)row & 15), end = off + cols * (int)sizeof(T);
     const char* const base = reinterpret_cast<const char*>(row) - off;
-    const uint32_t to = smem_u32(buf);
+    const uint32_t to = shared_address(buf);
     const int head = (off + 15) >> 4, tail = end >> 4;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
@@ -187,31 +177,6 @@ __device__ __forceinline__ void store_odd(const T* row, int cols, char* buf, int
   const int at = t == 0 ? 0 : cols - 1;
   const bool mine = t == 0 ? off & 1 : t == 1 && ((off + cols) & 1);
   if (mine) reinterpret_cast<uint16_t*>(buf)[off + at] = v;
-}
-
-typedef unsigned long long pair;        // two fp32 values
-__device__ __forceinline__ pair make_pair2(float a, float b) {
-  pair p;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(a), "f"(b));
-  return p;
-}
-__device__ __forceinline__ float first(pair p) { return __uint_as_float((uint32_t)p); }
-__device__ __forceinline__ float second(pair p) { return __uint_as_float((uint32_t)(p >> 32)); }
-__device__ __forceinline__ pair both(float a) { return make_pair2(a, a); }
-__device__ __forceinline__ pair add(pair a, pair b) {
-  pair d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ pair mul(pair a, pair b) {
-  pair d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ pair fma(pair a, pair b, pair c) {
-  pair d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
 }
 
 constexpr int log2_of(int n) { return n <= 1 ? 0 : 1 + log2_of(n / 2); }
