@@ -6,6 +6,7 @@ fails with instructions to build it.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import List, Optional, Sequence, Tuple
 
@@ -424,22 +425,30 @@ def _refuse(message: str):
     raise IstError(IST_ERR_ARG, message)
 
 
-def _call(device: torch.device, stream: Optional[torch.cuda.Stream], function, *args):
-    """function(*args, stream) with `device` current, on `stream` or the device's current stream."""
-    index = device.index
-    if stream is not None and stream.device_index != index:
-        _refuse(f"the stream belongs to another device than {device}")
-    if index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            return _call(device, stream, function, *args)
-    status = function(*args, (stream if stream is not None else torch.cuda.current_stream(index)).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _call(index: int, function, *args):
+    """function(*args, stream) with device `index` current, on that device's current stream."""
+    if index != _current_device():
+        with torch.cuda.device(index):
+            return _call(index, function, *args)
+    status = function(*args, _raw_stream(index))
     if status != IST_OK:
         raise IstError(status, lib.ist_last_error(None).decode())
 
 
-def _rows(t: torch.Tensor, name: str, cols: int, device: torch.device, rows: Optional[int] = None) -> Tuple[int, int, int]:
+def _on(stream: torch.cuda.Stream, tensor: torch.Tensor):
+    """Makes `stream` current: what a call allocates then belongs to the stream that it runs on."""
+    if stream.device != tensor.device:
+        _refuse(f"the stream belongs to another device than {tensor.device}")
+    return torch.cuda.stream(stream)
+
+
+def _rows(t: torch.Tensor, name: str, cols: int, index: int, rows: int = -1) -> Tuple[int, int, int]:
     """(element type, rows, stride) of a tensor whose last dimension is `cols` elements that lie together."""
-    if t.device != device or device.type != "cuda":
+    if t.get_device() != index or index < 0:
         _refuse(f"{name} is on {t.device}: one CUDA device for all tensors is needed")
     kind = _TYPES.get(t.dtype)
     if kind is None:
@@ -447,7 +456,7 @@ def _rows(t: torch.Tensor, name: str, cols: int, device: torch.device, rows: Opt
     if t.dim() == 0 or t.shape[-1] != cols or (cols > 1 and t.stride(-1) != 1):
         _refuse(f"{name}'s last dimension must be {cols} adjacent elements")
     n = t.numel() // cols
-    if rows is not None and n != rows:
+    if rows >= 0 and n != rows:
         _refuse(f"{name} has {n} rows, not {rows}")
     if n <= 1 or t.is_contiguous():
         return kind, n, cols
@@ -459,20 +468,27 @@ def _rows(t: torch.Tensor, name: str, cols: int, device: torch.device, rows: Opt
     return kind, n, t.stride(0)
 
 
-def _vector(t: Optional[torch.Tensor], name: str, count: int, device: torch.device) -> Optional[int]:
+def _vector(t: Optional[torch.Tensor], name: str, count: int, index: int) -> Optional[int]:
     if t is None:
         return None
-    if t.device != device or t.dtype != torch.float32 or t.numel() != count or not t.is_contiguous():
-        _refuse(f"{name} must be {count} contiguous fp32 values on {device}")
+    if t.get_device() != index or t.dtype != torch.float32 or t.numel() != count or not t.is_contiguous():
+        _refuse(f"{name} must be {count} contiguous fp32 values on the rows' device")
     return t.data_ptr()
 
 
-def _norm_shape(x: torch.Tensor, groups: int) -> Tuple[int, torch.device]:
+def _norm_shape(x: torch.Tensor, groups: int) -> Tuple[int, int]:
     if x.dim() == 0 or x.shape[-1] == 0:
         _refuse("x needs a last dimension of at least one element")
     if not 1 <= groups < 2 ** 31:
         _refuse("groups must be in 1..2^31 - 1")
-    return x.shape[-1], x.device
+    return x.shape[-1], x.get_device()
+
+
+def _like(x: torch.Tensor, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """An uninitialised contiguous tensor of x's shape."""
+    if x.is_contiguous():
+        return torch.empty_like(x) if dtype is None or dtype == x.dtype else torch.empty_like(x, dtype=dtype)
+    return torch.empty(x.shape, dtype=dtype if dtype is not None else x.dtype, device=x.device)
 
 
 def ist_layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
@@ -481,23 +497,31 @@ def ist_layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = Non
                            stream: Optional[torch.cuda.Stream] = None):
     """Layer norm over x's last dimension (fp32 or bf16; rows may have a stride).  weight, bias: fp32 [groups][cols], the
     rows belong in order to `groups` sites.  Returns (y, mean, rstd), y of y_dtype (default x's) or written into the tensor
-    `y`; mean and rstd are fp32 [rows], or None without want_stats."""
-    cols, dev = _norm_shape(x, groups)
-    x_type, rows, x_stride = _rows(x, "x", cols, dev)
+    `y`; mean and rstd are fp32 [rows], or None without want_stats.  Runs on `stream` or the device's current stream."""
+    if stream is not None:
+        with _on(stream, x):
+            return ist_layer_norm_forward(x, weight, bias, eps, groups, y, y_dtype, want_stats)
+    cols, index = _norm_shape(x, groups)
+    x_type, rows, x_stride = _rows(x, "x", cols, index)
     if y is None:
-        with torch.cuda.stream(stream):      # what a call allocates belongs to the stream it runs on
-            y = torch.empty(x.shape, dtype=y_dtype if y_dtype is not None else x.dtype, device=dev)
+        y = _like(x, y_dtype)
     elif y_dtype is not None and y.dtype != y_dtype:
         _refuse(f"y is {y.dtype}, not {y_dtype}")
-    y_type, _, y_stride = _rows(y, "y", cols, dev, rows)
-    mean = rstd = None
+    y_type, _, y_stride = _rows(y, "y", cols, index, rows)
+    mean = rstd = mean_at = rstd_at = None
     if want_stats:
-        with torch.cuda.stream(stream):
-            mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
-    _call(dev, stream, lib.ist_layer_norm_forward, x.data_ptr(), x_type, x_stride, rows, cols, groups,
-          _vector(weight, "weight", groups * cols, dev), _vector(bias, "bias", groups * cols, dev), eps, y.data_ptr(), y_type,
-          y_stride, _ptr(mean), _ptr(rstd))
+        mean = torch.empty(rows, dtype=torch.float32, device=index)
+        rstd = torch.empty(rows, dtype=torch.float32, device=index)
+        mean_at, rstd_at = mean.data_ptr(), rstd.data_ptr()
+    _call(index, lib.ist_layer_norm_forward, x.data_ptr(), x_type, x_stride, rows, cols, groups,
+          _vector(weight, "weight", groups * cols, index), _vector(bias, "bias", groups * cols, index), eps, y.data_ptr(), y_type,
+          y_stride, mean_at, rstd_at)
     return y, mean, rstd
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_workspace(rows: int, cols: int, groups: int) -> int:
+    return int(lib.ist_layer_norm_workspace_bytes(rows, cols, groups))
 
 
 def ist_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor,
@@ -506,31 +530,36 @@ def ist_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[
                             stream: Optional[torch.cuda.Stream] = None):
     """(dx, dweight, dbias) from the gradient of ist_layer_norm_forward's output and what that call read and returned; dx
     has x's type (or is written into the tensor `dx`), the others are fp32 [groups][cols], None where not wanted."""
-    cols, dev = _norm_shape(x, groups)
-    x_type, rows, x_stride = _rows(x, "x", cols, dev)
-    dy_type, _, dy_stride = _rows(dy, "dy", cols, dev, rows)
-    dx_stride = 0
+    if stream is not None:
+        with _on(stream, x):
+            return ist_layer_norm_backward(dy, x, weight, mean, rstd, groups, want_dx, want_dweight, want_dbias, dx)
+    cols, index = _norm_shape(x, groups)
+    x_type, rows, x_stride = _rows(x, "x", cols, index)
+    dy_type, _, dy_stride = _rows(dy, "dy", cols, index, rows)
     if dx is not None:
         if dx.dtype != x.dtype:
             _refuse("dx must have x's dtype")
     elif want_dx:
-        with torch.cuda.stream(stream):
-            dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        dx = _like(x)
+    dx_at = dweight_at = dbias_at = workspace_at = dweight = dbias = None
+    dx_stride = nbytes = 0
     if dx is not None:
-        _, _, dx_stride = _rows(dx, "dx", cols, dev, rows)
-    dweight = dbias = workspace = None
-    nbytes = 0
-    with torch.cuda.stream(stream):
-        if want_dweight:
-            dweight = torch.empty((groups, cols), dtype=torch.float32, device=dev)
-        if want_dbias:
-            dbias = torch.empty((groups, cols), dtype=torch.float32, device=dev)
-        if want_dweight or want_dbias:
-            nbytes = lib.ist_layer_norm_workspace_bytes(rows, cols, groups)
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    _call(dev, stream, lib.ist_layer_norm_backward, dy.data_ptr(), dy_type, dy_stride, x.data_ptr(), x_type, x_stride, rows, cols,
-          groups, _vector(weight, "weight", groups * cols, dev), _vector(mean, "mean", rows, dev),
-          _vector(rstd, "rstd", rows, dev), _ptr(dx), dx_stride, _ptr(dweight), _ptr(dbias), _ptr(workspace), nbytes)
+        _, _, dx_stride = _rows(dx, "dx", cols, index, rows)
+        dx_at = dx.data_ptr()
+    if want_dweight:
+        dweight = torch.empty((groups, cols), dtype=torch.float32, device=index)
+        dweight_at = dweight.data_ptr()
+    if want_dbias:
+        dbias = torch.empty((groups, cols), dtype=torch.float32, device=index)
+        dbias_at = dbias.data_ptr()
+    if want_dweight or want_dbias:
+        nbytes = _norm_workspace(rows, cols, groups)
+        if nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=index)
+            workspace_at = workspace.data_ptr()
+    _call(index, lib.ist_layer_norm_backward, dy.data_ptr(), dy_type, dy_stride, x.data_ptr(), x_type, x_stride, rows, cols, groups,
+          _vector(weight, "weight", groups * cols, index), _vector(mean, "mean", rows, index),
+          _vector(rstd, "rstd", rows, index), dx_at, dx_stride, dweight_at, dbias_at, workspace_at, nbytes)
     return dx, dweight, dbias
 
 
@@ -558,7 +587,9 @@ class AdamW:
             _refuse(f"parameters are on {dev}: a CUDA device is needed")
         if state_bits not in (8, 32):
             _refuse("state_bits is 32 or 8")
-        self.lr, self.steps, self.stream = float(lr), int(step), stream
+        self.lr, self.steps, self.stream, self.index = float(lr), int(step), stream, dev.index
+        if stream is not None and stream.device != dev:
+            _refuse(f"the stream belongs to another device than {dev}")
         self.sizes = [p.numel() for p in self.params]
         room = [-(-n // IST_ADAMW_BLOCK) * IST_ADAMW_BLOCK for n in self.sizes]
         self.offsets = [0]
@@ -601,7 +632,7 @@ class AdamW:
         for name, t, dtype in (("step_dev", step_dev, torch.int64), ("lr_dev", lr_dev, torch.float32)):
             if t is not None and (t.device != dev or t.dtype != dtype or t.numel() != 1):
                 _refuse(f"{name} must be one value of {dtype} on {dev}")
-        self.step_dev, self.lr_dev = step_dev, lr_dev
+        self.step_dev, self.lr_dev, self.table_at = step_dev, lr_dev, self.table.ctypes.data
         self.args = AdamWArgs(lr=self.lr, beta1=betas[0], beta2=betas[1], eps=eps, max_norm=max_norm or 0.0,
                               seed=seed & (2 ** 64 - 1), state_bits=state_bits, step_dev=_ptr(step_dev), lr_dev=_ptr(lr_dev))
         self.workspace = None
@@ -613,20 +644,24 @@ class AdamW:
         """One step with `grads` (default: the parameters' .grad), all fp32 or all bf16; a None passes its tensor over.
         Returns the gradients' norm (fp32 [1]) if they are clipped.  The gradients may be freed or written once the
         work on the stream that follows allows it, as with any asynchronous call."""
+        if self.stream is not None and _raw_stream(self.index) != self.stream.cuda_stream:
+            with torch.cuda.stream(self.stream):
+                return self.step(grads, lr)
         if grads is None:
             grads = [p.grad for p in self.params]
-        if len(grads) != len(self.params):
+        if len(grads) != len(self.sizes):
             _refuse("one gradient (or None) per parameter is needed")
-        dev, dtype, at = self.device, None, []
-        for i, (g, n) in enumerate(zip(grads, self.sizes)):
+        index, dtype, at = self.index, None, []
+        for g, n in zip(grads, self.sizes):
             if g is None:
                 at.append(0)
                 continue
-            dtype = dtype or g.dtype
-            if g.dtype != dtype or g.numel() != n or g.device != dev or not g.is_contiguous():
-                _refuse(f"gradient {i} must be {n} contiguous values of {dtype} on {dev}")
+            if dtype is None:
+                dtype = g.dtype
+            if g.dtype != dtype or g.numel() != n or g.get_device() != index or not g.is_contiguous():
+                _refuse(f"gradient {len(at)} must be {n} contiguous values of {dtype} on {self.device}")
             at.append(g.data_ptr())
-        kind = _TYPES.get(dtype, IST_T_F32 if dtype is None else None)
+        kind = IST_T_F32 if dtype is None else _TYPES.get(dtype)
         if kind is None:
             raise TypeError(f"unsupported gradient dtype {dtype}")
         self.table["grad"] = at
@@ -635,16 +670,14 @@ class AdamW:
         if lr is not None:
             self.lr = float(lr)
         args.lr, args.step = self.lr, self.steps + 1
-        norm = None
+        norm = workspace_at = None
         if self.workspace is not None:
-            with torch.cuda.stream(self.stream):
-                norm = torch.empty(1, dtype=torch.float32, device=dev)
+            workspace_at = self.workspace.data_ptr()
+            norm = torch.empty(1, dtype=torch.float32, device=index)
             args.norm_out_dev = norm.data_ptr()
         if self.step_dev is not None:
-            with torch.cuda.stream(self.stream):        # None: the current stream stays
-                self.step_dev.add_(1)
-        _call(dev, self.stream, lib.ist_adamw_step, self.table.ctypes.data, len(self.params), args, _ptr(self.workspace),
-              self.workspace_bytes)
+            self.step_dev.add_(1)
+        _call(index, lib.ist_adamw_step, self.table_at, len(at), args, workspace_at, self.workspace_bytes)
         self.steps += 1
         return norm
 
@@ -652,13 +685,13 @@ class AdamW:
         """First and second moments as flat tensors of `dtype` (fp32 or bf16), tensor i from offsets[i] on."""
         if dtype not in _TYPES:
             raise TypeError(f"unsupported dtype {dtype}")
+        if self.stream is not None and _raw_stream(self.index) != self.stream.cuda_stream:
+            with torch.cuda.stream(self.stream):
+                return self.state_values(dtype)
         m, v = self.state["exp_avg"], self.state["exp_avg_sq"]
         if "exp_avg_base" not in self.state:
-            with torch.cuda.stream(self.stream):
-                return m.to(dtype, copy=True), v.to(dtype, copy=True)
-        with torch.cuda.stream(self.stream):
-            out = torch.empty((2, m.numel()), dtype=dtype, device=self.device)
-        a, b = out.unbind(0)
-        _call(self.device, self.stream, lib.ist_adamw_state_values, m.data_ptr(), self.state["exp_avg_base"].data_ptr(),
-              v.data_ptr(), self.state["exp_avg_sq_base"].data_ptr(), m.numel(), _TYPES[dtype], a.data_ptr(), b.data_ptr())
+            return m.to(dtype, copy=True), v.to(dtype, copy=True)
+        a, b = torch.empty_like(m, dtype=dtype), torch.empty_like(v, dtype=dtype)
+        _call(self.index, lib.ist_adamw_state_values, m.data_ptr(), self.state["exp_avg_base"].data_ptr(), v.data_ptr(),
+              self.state["exp_avg_sq_base"].data_ptr(), m.numel(), _TYPES[dtype], a.data_ptr(), b.data_ptr())
         return a, b

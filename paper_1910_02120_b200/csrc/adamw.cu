@@ -16,7 +16,8 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kChunk = 2048;                     // values that a block takes at a time
 constexpr int kBlock = IST_ADAMW_BLOCK;          // values of an 8-bit state that share a base
 constexpr int kNormBlocks = 1184;                // at most, per launch: each leaves one partial sum
-constexpr int kSmallTable = 16, kTable = 400;    // tensors of a launch: the table is a kernel parameter (32,764 bytes at most)
+// Tensors of a launch.  The table is a kernel parameter, which may be 32,764 bytes; launches of up to 4 KB cost the host least.
+constexpr int kSmallTable = 16, kMiddleTable = 50, kTable = 400;
 
 struct Entry {
   float* p;
@@ -723,8 +724,9 @@ extern "C" ist_status ist_adamw_step(const ist_adamw_tensor* tensors_host, int64
     k.max_norm = args->max_norm;
     k.norm_out = args->norm_out_dev;
     double* const partials = clip ? (double*)workspace_dev : nullptr;
-    e = live <= kSmallTable ? step_launches<kSmallTable>(tensors_host, count, values, *args, k, partials, stream)
-                            : step_launches<kTable>(tensors_host, count, values, *args, k, partials, stream);
+    e = live <= kSmallTable    ? step_launches<kSmallTable>(tensors_host, count, values, *args, k, partials, stream)
+        : live <= kMiddleTable ? step_launches<kMiddleTable>(tensors_host, count, values, *args, k, partials, stream)
+                               : step_launches<kTable>(tensors_host, count, values, *args, k, partials, stream);
   }
   if (e != cudaSuccess) return fail_call(IST_ERR_CUDA, "ist_adamw_step: %s", cudaGetErrorString(e));
   return IST_OK;
