@@ -382,7 +382,7 @@ enum { IST_T_F32 = 0, IST_T_BF16 = 1 };
  * mean_out_dev, rstd_out_dev: [rows] fp32 for the backward pass, either may be NULL.  Statistics are taken
  * in fp32 or wider from the elements' values; y is rounded once, to nearest even.  A row that holds an infinity or
  * a NaN comes out as NaN, other rows are not touched by it.  rows = 0 is allowed.  0 < eps < inf.
- * 1 <= cols <= 2^30, 0 <= rows < 2^31, 1 <= groups < 2^31.  Outputs must not overlap inputs or one another
+ * 1 <= cols <= 2^30, 0 <= rows <= 2^31 - 65536, 1 <= groups < 2^31.  Outputs must not overlap inputs or one another
  * (rows of one buffer that interleave without sharing elements are fine).  Elements between the rows are left as they are.
  */
 ist_status ist_layer_norm_forward(const void* x_dev, int x_type, int64_t x_stride, int64_t rows, int64_t cols,

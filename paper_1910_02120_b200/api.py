@@ -632,9 +632,11 @@ class AdamW:
         for name, t, dtype in (("step_dev", step_dev, torch.int64), ("lr_dev", lr_dev, torch.float32)):
             if t is not None and (t.device != dev or t.dtype != dtype or t.numel() != 1):
                 _refuse(f"{name} must be one value of {dtype} on {dev}")
-        self.step_dev, self.lr_dev, self.table_at = step_dev, lr_dev, self.table.ctypes.data
+        self.step_dev, self.lr_dev = step_dev, lr_dev
+        self.table_at, self.words = self.table.ctypes.data, memoryview(self.table.view(np.uint64))
         self.args = AdamWArgs(lr=self.lr, beta1=betas[0], beta2=betas[1], eps=eps, max_norm=max_norm or 0.0,
                               seed=seed & (2 ** 64 - 1), state_bits=state_bits, step_dev=_ptr(step_dev), lr_dev=_ptr(lr_dev))
+        self.written = self.params + (self.copies or [])
         self.workspace = None
         self.workspace_bytes = int(lib.ist_adamw_workspace_bytes(len(self.params))) if max_norm else 0
         if max_norm:
@@ -651,20 +653,20 @@ class AdamW:
             grads = [p.grad for p in self.params]
         if len(grads) != len(self.sizes):
             _refuse("one gradient (or None) per parameter is needed")
-        index, dtype, at = self.index, None, []
+        index, dtype, words, at = self.index, None, self.words, 1      # the table's second word is the gradient's address
         for g, n in zip(grads, self.sizes):
             if g is None:
-                at.append(0)
-                continue
-            if dtype is None:
-                dtype = g.dtype
-            if g.dtype != dtype or g.numel() != n or g.get_device() != index or not g.is_contiguous():
-                _refuse(f"gradient {len(at)} must be {n} contiguous values of {dtype} on {self.device}")
-            at.append(g.data_ptr())
+                words[at] = 0
+            else:
+                if dtype is None:
+                    dtype = g.dtype
+                if g.dtype is not dtype or g.numel() != n or g.get_device() != index or not g.is_contiguous():
+                    _refuse(f"gradient {at // 9} must be {n} contiguous values of {dtype} on {self.device}")
+                words[at] = g.data_ptr()
+            at += 9
         kind = IST_T_F32 if dtype is None else _TYPES.get(dtype)
         if kind is None:
             raise TypeError(f"unsupported gradient dtype {dtype}")
-        self.table["grad"] = at
         args = self.args
         args.grad_type = kind
         if lr is not None:
@@ -677,8 +679,9 @@ class AdamW:
             args.norm_out_dev = norm.data_ptr()
         if self.step_dev is not None:
             self.step_dev.add_(1)
-        _call(index, lib.ist_adamw_step, self.table_at, len(at), args, workspace_at, self.workspace_bytes)
+        _call(index, lib.ist_adamw_step, self.table_at, len(self.sizes), args, workspace_at, self.workspace_bytes)
         self.steps += 1
+        torch.autograd.graph.increment_version(self.written)    # a graph that still needs the old values is told
         return norm
 
     def state_values(self, dtype: torch.dtype = torch.float32) -> Tuple[torch.Tensor, torch.Tensor]:

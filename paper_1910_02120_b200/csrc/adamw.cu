@@ -289,7 +289,7 @@ __device__ __noinline__ uint32_t largest_number(uint4 bits) {
 // into registers cannot be waited for one after the other: 131 us for 20 M values with one block of loads ahead, TODO us
 // this way).  Instructions, most of them integer ones, are what bounds the kernel then.  So blocks whose values are all finite
 // and none near fp32's largest, which is to say all of a healthy run's, take a path without the cases of the others.
-constexpr int kMostPer = 16, kStages = 4;
+constexpr int kMostPer = 16, kStages = 3;
 
 template <bool TINY, typename GT, int CAP>
 __device__ __forceinline__ void adamw8_chunks(const Table<CAP>& t, const Args& a, const Step& s, char* ring) {
@@ -439,7 +439,7 @@ __device__ __forceinline__ void adamw8_chunks(const Table<CAP>& t, const Args& a
 }
 
 template <typename GT, int CAP>
-__global__ void __launch_bounds__(kThreads, 3) adamw8_kernel(const __grid_constant__ Table<CAP> t, const Args a) {
+__global__ void __launch_bounds__(kThreads, 4) adamw8_kernel(const __grid_constant__ Table<CAP> t, const Args a) {
   extern __shared__ __align__(128) char rings[];
   char* const ring = rings + (threadIdx.x >> 5) * (kStages * kBlock * (4 + sizeof(GT) + 2));
   pdl_wait();

@@ -212,7 +212,8 @@ const char* bad_rows(const void* p, int type, int64_t stride, int64_t rows, int6
 }
 const char* bad_shape(int64_t rows, int64_t cols, int groups) {
   if (cols < 1 || cols > (int64_t)1 << 30) return "cols must be in 1..2^30";
-  if (rows < 0 || rows >= (int64_t)1 << 31) return "rows must be in 0..2^31 - 1";
+  // row numbers are 32-bit, and run a few tiles past the last row
+  if (rows < 0 || rows > ((int64_t)1 << 31) - 65536) return "rows must be in 0..2^31 - 65536";
   if (groups < 1 || rows % groups) return "groups must be >= 1 and divide rows";
   if (cols > ((int64_t)1 << 40) / groups) return "groups * cols must be at most 2^40";
   return nullptr;

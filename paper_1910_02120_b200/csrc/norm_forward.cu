@@ -267,9 +267,12 @@ bool dispatch(const NormForward& a, cudaStream_t stream, cudaError_t* e) {
     TAKE(0, 1, 2, 8, 4, 3, 1);
     TAKE(17, 1, 2, 32, 4, 3, 1);
     TAKE(65, 1, 8, 32, 4, 3, 1);
-    TAKE(257, 1, 16, 32, 2, 3, 1);
-    TAKE(513, 1, 16, 64, 2, 3, 1);
-    TAKE(1025, 1, 16, 128, 2, 3, 1);
+    TAKE(257, 1, 12, 32, 1, 4, 1);
+    TAKE(385, 1, 16, 32, 1, 4, 1);
+    TAKE(513, 1, 12, 64, 1, 4, 1);
+    TAKE(769, 1, 16, 64, 1, 4, 1);
+    TAKE(1025, 1, 12, 128, 1, 4, 1);
+    TAKE(1537, 1, 16, 128, 1, 4, 1);
     TAKE(2049, 1, 16, 256, 2, 3, 1);
     TAKE(4097, 1, 16, 512, 2, 2, 1);
     TAKE(8193, 1, 32, 512, 1, 3, 1);

@@ -420,3 +420,11 @@ def test_refusals(api):
     with pytest.raises(TypeError):
         opt.state_values(torch.float16)
     assert not p.any() and opt.steps == 0
+
+
+def test_a_step_tells_graphs_that_need_the_old_values(api):
+    p = torch.ones(8, device=DEV, requires_grad=True)
+    loss = (p * p).sum()
+    api.AdamW([p]).step([torch.ones(8, device=DEV)])
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()

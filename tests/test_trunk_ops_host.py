@@ -26,7 +26,7 @@ def _forward(api, x=P, x_type=0, x_stride=8, rows=4, cols=8, groups=2, weight=No
 
 @pytest.mark.parametrize("bad, word", [
     (dict(x=None), "null"), (dict(y=None), "null"), (dict(x_type=2), "types"), (dict(y_type=-1), "types"),
-    (dict(rows=-1), "rows"), (dict(rows=1 << 31, groups=1), "rows"), (dict(cols=0), "cols"), (dict(cols=(1 << 30) + 1), "cols"),
+    (dict(rows=-1), "rows"), (dict(rows=1 << 31, groups=1), "rows"), (dict(rows=(1 << 31) - 65535, groups=1), "rows"), (dict(cols=0), "cols"), (dict(cols=(1 << 30) + 1), "cols"),
     (dict(groups=0), "groups"), (dict(groups=3), "groups"), (dict(x_stride=7), "stride"), (dict(y_stride=0), "stride"),
     (dict(x_stride=(1 << 40) + 1), "stride"), (dict(rows=1 << 20, x_stride=1 << 40), "stride"), (dict(eps=0.0), "eps"),
     (dict(eps=math.inf), "eps"), (dict(eps=math.nan), "eps"), (dict(eps=-1.0), "eps"), (dict(x=P + 2), "aligned"),
