@@ -329,8 +329,8 @@ __device__ __forceinline__ void adamw8_chunks(const Table<CAP>& t, const Args& a
 #pragma unroll
       for (int k = 0; k < 4; k += 2) {
         const pair gc = mul(make_pair2(gf[k], gf[k + 1]), clip);
-        const pair mn = add(mul(b1, make_pair2(mf[k], mf[k + 1])), mul(c1, gc));
-        const pair vn = add(mul(b2, make_pair2(vf[k], vf[k + 1])), mul(mul(c2, gc), gc));
+        const pair mn = add_rounded(mul(b1, make_pair2(mf[k], mf[k + 1])), mul(c1, gc));
+        const pair vn = add_rounded(mul(b2, make_pair2(vf[k], vf[k + 1])), mul(mul(c2, gc), gc));
         const pair d = fma(make_pair2(root_of<TINY>(first_of(vn)), root_of<TINY>(second_of(vn))), inv_root, eps);
         const pair q = mul(mn, make_pair2(inverse(first_of(d)), inverse(second_of(d))));
         const pair po = make_pair2(pf[k], pf[k + 1]), pn = fma(step, q, fma(decay, po, po));

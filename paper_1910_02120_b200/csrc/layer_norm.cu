@@ -224,7 +224,10 @@ const char* bad_shape(int64_t rows, int64_t cols, int groups) {
 int parts_of(int64_t rows, int64_t cols, int groups) {
   const int64_t site_rows = rows / groups;
   int64_t parts, least;
-  if (cols <= kNormWidest) {
+  if (cols <= kNormNarrow) {
+    parts = (int64_t)sm_count() * 4 / groups;
+    least = 4 * kNormThreads;
+  } else if (cols <= kNormWidest) {
     parts = (int64_t)sm_count() * (cols <= 256 ? 2 : 1) / norm_cluster(cols) / groups;
     least = ceil_div(16384, cols);
   } else {

@@ -168,7 +168,11 @@ __global__ void __launch_bounds__(NV * V == 16 ? 512 : kNormThreads) norm_backwa
             for (int e = 0; e < kPairs; ++e) {
               const int q = i * V / 2 + e;
               const pair h = mul(add(make_pair2(xv[2 * e], xv[2 * e + 1]), minus), rs);
-              const pair o = mul(fma(h, m1, fma(make_pair2(dv[2 * e], dv[2 * e + 1]), w[q], m0)), rs);
+              const pair d = make_pair2(dv[2 * e], dv[2 * e + 1]);
+              // rows of one or two elements have next to nothing left after the subtractions: there (V = 1) every product is
+              // rounded as it was for the sums, so that what cancels does
+              const pair o = V == 1 ? mul(add_rounded(add_rounded(mul(d, w[q]), m0), mul(h, m1)), rs)
+                                    : mul(fma(h, m1, fma(d, w[q], m0)), rs);
               xv[2 * e] = first_of(o);
               xv[2 * e + 1] = second_of(o);
             }
@@ -258,7 +262,8 @@ bool dispatch(const NormBackward& a, cudaStream_t stream, cudaError_t* e) {
   // two tiles in use and one or two on their way, in the shared memory of two blocks (or one of 512 threads)
   constexpr int S = sizeof(XT) + sizeof(DT), D = S == 6 ? 4 : 3, R = S == 4 ? 2 : 1;
   if (pieces) {
-    TAKE(0, V, 1, 64 / V, 4, 3, 1);
+    TAKE(0, V, 1, 32 / V, 4, 3, 1);
+    TAKE(33, V, 1, 64 / V, 4, 3, 1);
     TAKE(65, V, 1, 128 / V, 4, 3, 1);
     TAKE(129, V, 8 / V, 32, 4, 3, 1);
     TAKE(257, V, 16 / V, 32, R, D, 1);
@@ -270,9 +275,10 @@ bool dispatch(const NormBackward& a, cudaStream_t stream, cudaError_t* e) {
     TAKE(0, V, 16 / V, 512, R, D, 4);
     TAKE(0, V, 16 / V, 512, R, D, 8);
   } else {
-    TAKE(0, 1, 2, 8, 4, 3, 1);
-    TAKE(17, 1, 2, 32, 4, 3, 1);
-    TAKE(65, 1, 8, 32, 4, 3, 1);
+    TAKE(0, 1, 4, 8, 4, 3, 1);
+    TAKE(33, 1, 8, 8, 2, 3, 1);
+    TAKE(65, 1, 8, 16, 2, 3, 1);
+    TAKE(129, 1, 8, 32, 2, 3, 1);
     TAKE(257, 1, 16, 32, R, D, 1);
     TAKE(513, 1, 16, 64, R, D, 1);
     TAKE(1025, 1, 16, 128, R, D, 1);
@@ -289,6 +295,7 @@ bool dispatch(const NormBackward& a, cudaStream_t stream, cudaError_t* e) {
 }  // namespace
 
 bool norm_backward_rows(const NormBackward& a, bool x_bf16, bool dy_bf16, cudaStream_t stream, cudaError_t* e) {
+  if (a.cols <= kNormNarrow) return *e = norm_backward_narrow(a, x_bf16, dy_bf16, stream), true;
   return x_bf16 ? dy_bf16 ? dispatch<bf16, bf16>(a, stream, e) : dispatch<bf16, float>(a, stream, e)
                 : dy_bf16 ? dispatch<float, bf16>(a, stream, e) : dispatch<float, float>(a, stream, e);
 }

@@ -252,7 +252,8 @@ bool dispatch(const NormForward& a, cudaStream_t stream, cudaError_t* e) {
     return *e = launch<XT, YT, v, nv, tpr, rb, d, cl, (v) * (nv) * (tpr)>(a, stream), true;               \
   if (n <= (v) * (nv) * (tpr) * (cl)) return *e = launch<XT, YT, v, nv, tpr, rb, d, cl, least>(a, stream), true
   if (pieces) {
-    TAKE(0, V, 1, 64 / V, 4, 3, 1);
+    TAKE(0, V, 1, 32 / V, 4, 3, 1);
+    TAKE(33, V, 1, 64 / V, 4, 3, 1);
     TAKE(65, V, 1, 128 / V, 4, 3, 1);
     TAKE(129, V, 8 / V, 32, 4, 3, 1);
     TAKE(257, V, 16 / V, 32, 2, 3, 1);
@@ -264,9 +265,10 @@ bool dispatch(const NormForward& a, cudaStream_t stream, cudaError_t* e) {
     TAKE(0, V, 32 / V, 512, 1, 3, 2);
     TAKE(0, V, 32 / V, 512, 1, 3, 4);
   } else {
-    TAKE(0, 1, 2, 8, 4, 3, 1);
-    TAKE(17, 1, 2, 32, 4, 3, 1);
-    TAKE(65, 1, 8, 32, 4, 3, 1);
+    TAKE(0, 1, 4, 8, 4, 3, 1);
+    TAKE(33, 1, 8, 8, 4, 3, 1);
+    TAKE(65, 1, 8, 16, 4, 3, 1);
+    TAKE(129, 1, 8, 32, 4, 3, 1);
     TAKE(257, 1, 12, 32, 1, 4, 1);
     TAKE(385, 1, 16, 32, 1, 4, 1);
     TAKE(513, 1, 12, 64, 1, 4, 1);
@@ -286,6 +288,7 @@ bool dispatch(const NormForward& a, cudaStream_t stream, cudaError_t* e) {
 }  // namespace
 
 bool norm_forward_rows(const NormForward& a, bool x_bf16, bool y_bf16, cudaStream_t stream, cudaError_t* e) {
+  if (a.cols <= kNormNarrow) return *e = norm_forward_narrow(a, x_bf16, y_bf16, stream), true;
   return x_bf16 ? y_bf16 ? dispatch<bf16, bf16>(a, stream, e) : dispatch<bf16, float>(a, stream, e)
                 : y_bf16 ? dispatch<float, bf16>(a, stream, e) : dispatch<float, float>(a, stream, e);
 }

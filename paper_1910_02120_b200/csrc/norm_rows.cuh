@@ -51,7 +51,10 @@ struct NormBackward {
 // norm_forward.cu, norm_backward.cu: false if no kernel takes rows of this width (nothing is launched).
 bool norm_forward_rows(const NormForward& a, bool x_bf16, bool y_bf16, cudaStream_t stream, cudaError_t* e);
 bool norm_backward_rows(const NormBackward& a, bool x_bf16, bool dy_bf16, cudaStream_t stream, cudaError_t* e);
-constexpr int kNormWidest = 65536;
+// norm_narrow.cu: rows of up to kNormNarrow elements.
+cudaError_t norm_forward_narrow(const NormForward& a, bool x_bf16, bool y_bf16, cudaStream_t stream);
+cudaError_t norm_backward_narrow(const NormBackward& a, bool x_bf16, bool dy_bf16, cudaStream_t stream);
+constexpr int kNormNarrow = 16, kNormWidest = 65536;
 // Blocks of a cluster that share a row of the second one.
 inline int norm_cluster(int64_t cols) { return cols <= 8192 ? 1 : cols <= 16384 ? 2 : cols <= 32768 ? 4 : 8; }
 
@@ -127,10 +130,12 @@ __device__ __forceinline__ void load_vector(const float* p, bool wide, float* v)
 __host__ __device__ __forceinline__ constexpr int part_width(int cols, int cl) {
   return cl == 1 ? cols : ((cols + cl - 1) / cl + 7) / 8 * 8;
 }
-// A row's bytes in shared memory: room for its 16-byte pieces, whatever its offset from a boundary, in whole lines of 128
-// bytes (a warp's access that starts inside a line takes one turn more: fp32 rows of 1024, forward, 33 us and 39 us).
+// A row's bytes in shared memory: room for its 16-byte pieces, whatever its offset from a boundary.  Rows that are copied in wide
+// pieces by a warp or more take whole lines of 128 bytes (a warp's access that starts inside a line takes one turn more:
+// fp32 rows of 1024, forward, 33 us and 39 us).
 __host__ __device__ __forceinline__ constexpr int row_room(int cols, int size, bool anywhere) {
-  return (cols * size + (anywhere ? 15 : 0) + 127) / 128 * 128;
+  const int bytes = cols * size, unit = bytes < 512 ? 16 : 128;
+  return (bytes + (anywhere ? 15 : 0) + unit - 1) / unit * unit;
 }
 
 // Starts the copies of a row into `buf`.  LEAST: columns that it has at least.

@@ -7,6 +7,8 @@
 namespace ist {
 namespace {
 
+// A product and a sum of pairs may be fused by the assembler, their rounding modifiers notwithstanding (seen in results).  Where
+// the product's own rounding counts, the sum is taken with add_rounded.
 typedef unsigned long long pair;        // two fp32 values
 __device__ __forceinline__ pair make_pair2(float a, float b) {
   pair p;
@@ -20,6 +22,9 @@ __device__ __forceinline__ pair add(pair a, pair b) {
   pair d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
+}
+__device__ __forceinline__ pair add_rounded(pair a, pair b) {
+  return make_pair2(__fadd_rn(first_of(a), first_of(b)), __fadd_rn(second_of(a), second_of(b)));
 }
 __device__ __forceinline__ pair mul(pair a, pair b) {
   pair d;

@@ -223,6 +223,19 @@ def test_a_row_that_is_not_finite_stays_alone(api, cols, bad):
         assert torch.equal(a[1], c[1]) and torch.equal(a[0, other], c[0, other]) and not a[0, cols // 2].isfinite()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_of_one_element(api, dtype):
+    """Their own mean: y is the bias, and nothing depends on x."""
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    x, _ = make_rows(1000, 1, dtype, gen)
+    w, b = vectors(4, 1, gen)
+    y, mean, rstd = api.ist_layer_norm_forward(x, w, b, groups=4, y_dtype=F32)
+    assert torch.equal(y, b.repeat_interleave(250, 0)) and torch.equal(mean, x[:, 0].float())
+    dy, _ = make_rows(1000, 1, F32, gen)
+    dx, dw, db = check_backward(api, dy, x, w, mean, rstd, 4)
+    assert not dx.any() and not dw.any()
+
+
 def test_same_bits_every_time(api):
     gen = torch.Generator(device=DEV).manual_seed(1)
     for rows, cols, groups in ((4096, 1024, 1), (1200, 1001, 6), (300, 16384, 2), (64, 40000, 1)):
