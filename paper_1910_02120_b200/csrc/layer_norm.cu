@@ -1,4 +1,14 @@
-// Layer normalisation of rows and its way back (ist_layer_norm_forward / _backward, see ist.h).
+// Layer normalisation of rows and its way back (ist_layer_norm_forward / _backward, see ist.h): argument checks, the choice of
+// kernels, and the kernels for what the others do not take.
+//
+//   up to 16 columns     norm_narrow.cu                   a thread takes a row
+//   up to 65,536         norm_forward.cu, _backward.cu    8 to 512 threads of a block, or a cluster of blocks, take a row, which is
+//                                                         read once; rows that are aligned to pieces of 16 bytes and those that are not
+//   wider                here                             a block takes a row and reads it again from L2; sums over rows in a launch of their own
+//
+// The sums over a site's rows for dweight and dbias are taken part by part, a block each, and the parts' sums are added by one more
+// launch (norm_join_kernel) in an order that the shape alone decides; no atomics.  All of it is bound by memory, and short
+// of that by issuing instructions, the more so the narrower the types and the less aligned the rows.
 #include "../../include/ist.h"
 
 #include <algorithm>
@@ -28,6 +38,7 @@ __device__ __forceinline__ double2 block_sum(double2 v, double2* sh) {
   return s;
 }
 
+// Rows of any width.  Sums in fp64: a thread adds hundreds of values one after the other.
 template <typename XT, typename YT>
 __global__ void __launch_bounds__(kThreads) norm_forward_any_kernel(const XT* x, int64_t x_ld, int64_t rows, int64_t cols,
                                                                    int64_t site_rows, const float* weight,

@@ -8,6 +8,9 @@
 namespace ist {
 namespace {
 
+// 51,200 rows of 1024, x bf16 and dy fp32: 72 us with the join, 0.89 of the copy rate; 4096 bf16 rows of 16384: 84 us, 0.74 (issuing
+// instructions); 9600 rows of 1001, which start anywhere: 28 us, against 21 us for 1000 columns.
+//
 // A tile is gone through twice: first for its sums, then, after the next tile's sums have been begun, for dx.  So the
 // shuffles and the barrier of one tile's sums run beside the arithmetic of another, at the price of unpacking the rows twice
 // (shared memory is not what bounds this) and of two tiles' rows kept.
@@ -259,6 +262,9 @@ bool dispatch(const NormBackward& a, cudaStream_t stream, cudaError_t* e) {
   if ((v) > 1 && n == (v) * (nv) * (tpr) * (cl))                                                           \
     return *e = launch<XT, DT, v, nv, tpr, rb, d, cl, (v) * (nv) * (tpr)>(a, stream), true;               \
   if (n <= (v) * (nv) * (tpr) * (cl)) return *e = launch<XT, DT, v, nv, tpr, rb, d, cl, least>(a, stream), true
+  // Sixteen columns a thread from 257 on, on 512 threads an SM: one block of 512 leaves half the parts' sums that two of 256 leave
+  // (rows of 4096, bf16: 47.6 us and 40.6 us).  Two rows at a time where a stage of both types is small (36.9 us against 41 us for
+  // bf16 rows of 1024), four rows up to 256 columns.
   // two tiles in use and one or two on their way, in the shared memory of two blocks (or one of 512 threads)
   constexpr int S = sizeof(XT) + sizeof(DT), D = S == 6 ? 4 : 3, R = S == 4 ? 2 : 1;
   if (pieces) {

@@ -61,8 +61,8 @@ inline int norm_cluster(int64_t cols) { return cols <= 8192 ? 1 : cols <= 16384 
 namespace {
 
 // Writes to the place in block `rank` of the cluster that corresponds to `at` in this one; the write itself tells that block's
-// barrier, so no fence stands behind it (a cluster barrier would wait for all of the threads' stores to global memory too:
-// rows of 16384 took 150 us that way and TODO us this way).
+// barrier, so no fence stands behind it (a cluster barrier would wait for all of the threads' stores to global memory too: 4096
+// bf16 rows of 16384 shared by four blocks, backward, 189 us that way and 161 us this way).
 __device__ __forceinline__ void send_cluster(float* at, uint64_t* bar, uint32_t rank, float v) {
   asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];"
                ::"r"(map_to_cta(at, rank)), "f"(v), "r"(map_to_cta(bar, rank)) : "memory");

@@ -203,8 +203,15 @@ def test_a_single_tensor(api, bits, n):
     check_step(api, [n], bits, steps=3, max_norm=1e-3)
 
 
+@pytest.mark.parametrize("grad", [F32, BF16])
+@pytest.mark.parametrize("offset", [0, 3])
+def test_large_tensors(api, grad, offset):
+    """More blocks of 128 values than the GPU holds at a time, several to a warp."""
+    check_step(api, [5000001, 300, 4000000, 129], 8, grad, copy=True, offset=offset, max_norm=1.0, steps=1)
+
+
 @pytest.mark.parametrize("bits", [32, 8])
-@pytest.mark.parametrize("count", [16, 17, 400, 401, 1300])
+@pytest.mark.parametrize("count", [16, 17, 50, 51, 400, 401, 1300])
 def test_many_tensors(api, bits, count):
     check_step(api, [1 + (7 * i) % 300 for i in range(count)], bits, steps=2, max_norm=2.0, scale=1e-4)
 

@@ -94,7 +94,7 @@ def check_backward(api, dy, x, w, mean, rstd, groups=1, dx_view=None, **kw):
 
 
 WIDTHS = [1, 2, 3, 7, 8, 31, 32, 33, 64, 100, 128, 129, 200, 255, 256, 257, 500, 512, 513, 768, 1000, 1001, 1024, 1025, 1500, 2048,
-          2049, 3001, 4096, 4100, 5000, 8192, 8200, 10007, 16384, 16392, 20000, 32768, 33000, 50001]
+          2049, 3001, 4096, 4100, 5000, 8192, 8200, 10007, 16384, 16392, 20000, 32768, 33000, 50001, 65536, 65537, 70003]
 
 
 @pytest.mark.parametrize("x_dtype, y_dtype", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
@@ -123,6 +123,20 @@ def test_rows_and_groups(api, rows, groups, cols, dtype):
     dx, dw, db = check_backward(api, dy, x, w, mean, rstd, groups)
     if rows == 0:
         assert not dw.any() and not db.any()
+
+
+@pytest.mark.parametrize("x_dtype, y_dtype", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("cols", [3, 16, 24, 33, 64, 100, 128, 250, 256, 500, 512, 700, 1000, 1001, 1024, 1500, 2048, 4001, 4096, 8192, 9000, 16384, 30001])
+def test_many_rows(api, cols, x_dtype, y_dtype):
+    """Enough rows for every block to go round its ring of stages several times, sites that end inside a tile among them."""
+    gen = torch.Generator(device=DEV).manual_seed(cols)
+    groups = 3
+    rows = groups * (2 ** 24 // cols // groups)
+    x, _ = make_rows(rows, cols, x_dtype, gen)
+    w, b = vectors(groups, cols, gen)
+    y, mean, rstd = check_forward(api, x, w, b, groups, y_dtype=y_dtype)
+    dy, _ = make_rows(rows, cols, y_dtype, gen, shift=0.0, scale=1e-2)
+    check_backward(api, dy, x, w, mean, rstd, groups)
 
 
 @pytest.mark.parametrize("offset, pad", [(0, 1), (1, 0), (1, 1), (2, 2), (4, 4), (4, 0), (3, 5), (8, 8)])
