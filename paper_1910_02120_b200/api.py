@@ -7,7 +7,9 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 import os
+from array import array
 from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
@@ -425,6 +427,7 @@ def _refuse(message: str):
     raise IstError(IST_ERR_ARG, message)
 
 
+_Tensor, _dtype_of = torch._C.TensorBase, operator.attrgetter("dtype")
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -505,9 +508,13 @@ def ist_layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = Non
     x_type, rows, x_stride = _rows(x, "x", cols, index)
     if y is None:
         y = _like(x, y_dtype)
-    elif y_dtype is not None and y.dtype != y_dtype:
-        _refuse(f"y is {y.dtype}, not {y_dtype}")
-    y_type, _, y_stride = _rows(y, "y", cols, index, rows)
+        y_type, y_stride = _TYPES.get(y.dtype, -1), cols
+        if y_type < 0:
+            raise TypeError(f"unsupported dtype {y.dtype} of y")
+    else:
+        if y_dtype is not None and y.dtype != y_dtype:
+            _refuse(f"y is {y.dtype}, not {y_dtype}")
+        y_type, _, y_stride = _rows(y, "y", cols, index, rows)
     mean = rstd = mean_at = rstd_at = None
     if want_stats:
         mean = torch.empty(rows, dtype=torch.float32, device=index)
@@ -536,15 +543,16 @@ def ist_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[
     cols, index = _norm_shape(x, groups)
     x_type, rows, x_stride = _rows(x, "x", cols, index)
     dy_type, _, dy_stride = _rows(dy, "dy", cols, index, rows)
+    dx_stride = cols
     if dx is not None:
         if dx.dtype != x.dtype:
             _refuse("dx must have x's dtype")
+        _, _, dx_stride = _rows(dx, "dx", cols, index, rows)
     elif want_dx:
         dx = _like(x)
     dx_at = dweight_at = dbias_at = workspace_at = dweight = dbias = None
-    dx_stride = nbytes = 0
+    nbytes = 0
     if dx is not None:
-        _, _, dx_stride = _rows(dx, "dx", cols, index, rows)
         dx_at = dx.data_ptr()
     if want_dweight:
         dweight = torch.empty((groups, cols), dtype=torch.float32, device=index)
@@ -633,7 +641,7 @@ class AdamW:
             if t is not None and (t.device != dev or t.dtype != dtype or t.numel() != 1):
                 _refuse(f"{name} must be one value of {dtype} on {dev}")
         self.step_dev, self.lr_dev = step_dev, lr_dev
-        self.table_at, self.words = self.table.ctypes.data, memoryview(self.table.view(np.uint64))
+        self.table_at, self.words = self.table.ctypes.data, memoryview(self.table.view(np.uint64)).cast("B").cast("Q")
         self.args = AdamWArgs(lr=self.lr, beta1=betas[0], beta2=betas[1], eps=eps, max_norm=max_norm or 0.0,
                               seed=seed & (2 ** 64 - 1), state_bits=state_bits, step_dev=_ptr(step_dev), lr_dev=_ptr(lr_dev))
         self.written = self.params + (self.copies or [])
@@ -653,17 +661,19 @@ class AdamW:
             grads = [p.grad for p in self.params]
         if len(grads) != len(self.sizes):
             _refuse("one gradient (or None) per parameter is needed")
-        index, dtype, words, at = self.index, None, self.words, 1      # the table's second word is the gradient's address
-        for g, n in zip(grads, self.sizes):
-            if g is None:
-                words[at] = 0
-            else:
-                if dtype is None:
-                    dtype = g.dtype
-                if g.dtype is not dtype or g.numel() != n or g.get_device() != index or not g.is_contiguous():
-                    _refuse(f"gradient {at // 9} must be {n} contiguous values of {dtype} on {self.device}")
-                words[at] = g.data_ptr()
-            at += 9
+        index, dtype = self.index, None
+        if type(None) in set(map(type, grads)):
+            given = [g for g in grads if g is not None]
+            sizes = [n for g, n in zip(grads, self.sizes) if g is not None]
+            self.words[1::9] = array("Q", [0 if g is None else g.data_ptr() for g in grads])
+        else:                                           # the table's second word of nine is the gradient's address
+            given, sizes = grads, self.sizes
+            self.words[1::9] = array("Q", map(_Tensor.data_ptr, grads))
+        if given:
+            dtype = given[0].dtype
+            if (list(map(_Tensor.numel, given)) != sizes or not all(map(_Tensor.is_contiguous, given))
+                    or set(map(_Tensor.get_device, given)) != {index} or len(set(map(_dtype_of, given))) != 1):
+                _refuse(f"gradients must be contiguous, of their parameters' sizes, of one dtype and on {self.device}")
         kind = IST_T_F32 if dtype is None else _TYPES.get(dtype)
         if kind is None:
             raise TypeError(f"unsupported gradient dtype {dtype}")

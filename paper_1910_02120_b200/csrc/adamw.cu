@@ -389,15 +389,17 @@ __device__ __forceinline__ void adamw8_chunks(const Table<CAP>& t, const Args& a
         out = lift_zeros4(out, make_uint4(vbits[0], vbits[1], vbits[2], vbits[3]));
       *vw = out;
     };
+    uint32_t in = 0, out = 0;                              // places in the ring of the next block to arrive and to be worked on
     auto fetch = [&](int u) {
       if (u < whole) {
-        char* const to = ring + (u % kStages) * kStage;
+        char* const to = ring + in;
         const uint32_t i = mine + u * kBlock;
         copy_async<16>(shared_address(to + lane * 16), p + i);
         copy_async<4 * sizeof(GT)>(shared_address(to + kBlock * 4 + lane * (4 * sizeof(GT))), g + i);
         copy_async<4>(shared_address(to + kBlock * (4 + sizeof(GT)) + lane * 4), m + i);
         copy_async<4>(shared_address(to + kBlock * (5 + sizeof(GT)) + lane * 4), v + i);
       }
+      in = in == (kStages - 1) * kStage ? 0 : in + kStage;
       copy_commit();
     };
 #pragma unroll
@@ -406,7 +408,8 @@ __device__ __forceinline__ void adamw8_chunks(const Table<CAP>& t, const Args& a
     for (int u = 0; u < whole; ++u) {
       fetch(u + kStages - 1);
       copy_wait<kStages - 1>();
-      const char* const from = ring + (u % kStages) * kStage;
+      const char* const from = ring + out;
+      out = out == (kStages - 1) * kStage ? 0 : out + kStage;
       float pf[4], gf[4];
       load4(reinterpret_cast<const float*>(from) + lane * 4, pf);
       load4(reinterpret_cast<const GT*>(from + kBlock * 4) + lane * 4, gf);
