@@ -381,7 +381,8 @@ enum { IST_T_F32 = 0, IST_T_BF16 = 1 };
  *   y_j = (x_j - mean) * rstd * weight_j + bias_j.
  * mean_out_dev, rstd_out_dev: [rows] fp32 for the backward pass, either may be NULL.  Statistics are taken
  * in fp32 or wider from the elements' values; y is rounded once, to nearest even.  A row that holds an infinity or
- * a NaN comes out as NaN, other rows are not touched by it.  rows = 0 is allowed.  0 < eps < inf.
+ * a NaN comes out as NaN, other rows are not touched by it.  Squares of a row's differences from its mean have to stay within
+ * fp32 (differences of up to about 1e18 in a row of a million elements).  rows = 0 is allowed.  0 < eps < inf.
  * 1 <= cols <= 2^30, 0 <= rows <= 2^31 - 65536, 1 <= groups < 2^31.  Outputs must not overlap inputs or one another
  * (rows of one buffer that interleave without sharing elements are fine).  Elements between the rows are left as they are.
  */
@@ -397,8 +398,8 @@ ist_status ist_layer_norm_forward(const void* x_dev, int x_type, int64_t x_strid
  * dx_out_dev, dweight_out_dev and dbias_out_dev may be NULL where they are not wanted (not all three).  The sums over rows
  * are added in an order that depends on the shape alone, so results are the same from call to call.  rows = 0 gives
  * zeros for dweight and dbias.  workspace_dev: at least ist_layer_norm_workspace_bytes(rows, cols, groups) bytes
- * (0 on invalid arguments), 16-byte aligned, not needed (may be NULL) if neither dweight nor dbias is wanted; its content means nothing before and
- * after the call.
+ * (0 where none is needed, and on invalid arguments, which the call then refuses), 16-byte aligned; may be NULL where none is needed or neither
+ * dweight nor dbias is wanted; its content means nothing before and after the call.
  */
 size_t ist_layer_norm_workspace_bytes(int64_t rows, int64_t cols, int groups);
 ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, int64_t dy_stride, const void* x_dev, int x_type,

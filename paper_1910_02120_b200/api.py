@@ -644,7 +644,7 @@ class AdamW:
         self.table_at, self.words = self.table.ctypes.data, memoryview(self.table.view(np.uint64)).cast("B").cast("Q")
         self.args = AdamWArgs(lr=self.lr, beta1=betas[0], beta2=betas[1], eps=eps, max_norm=max_norm or 0.0,
                               seed=seed & (2 ** 64 - 1), state_bits=state_bits, step_dev=_ptr(step_dev), lr_dev=_ptr(lr_dev))
-        self.written = self.params + (self.copies or [])
+        self.written = [t for t in self.params + (self.copies or []) if not t.is_inference()]
         self.workspace = None
         self.workspace_bytes = int(lib.ist_adamw_workspace_bytes(len(self.params))) if max_norm else 0
         if max_norm:
@@ -689,7 +689,12 @@ class AdamW:
             args.norm_out_dev = norm.data_ptr()
         if self.step_dev is not None:
             self.step_dev.add_(1)
-        _call(index, lib.ist_adamw_step, self.table_at, len(self.sizes), args, workspace_at, self.workspace_bytes)
+        try:
+            _call(index, lib.ist_adamw_step, self.table_at, len(self.sizes), args, workspace_at, self.workspace_bytes)
+        except IstError:
+            if self.step_dev is not None:               # a refused step is no step
+                self.step_dev.sub_(1)
+            raise
         self.steps += 1
         torch.autograd.graph.increment_version(self.written)    # a graph that still needs the old values is told
         return norm

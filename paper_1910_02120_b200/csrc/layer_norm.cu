@@ -196,16 +196,18 @@ struct Span {
   const void* p;
   int64_t rows, run, pitch;
 };
-// Whether two arrays share a byte.  Rows of equal pitch that lie side by side in one buffer do not.
+// Whether two arrays share a byte.  Rows of equal pitch that lie side by side in one buffer do not, nor does a single run that lies
+// between rows.
 bool overlap(const Span& a, const Span& b) {
   if (!a.p || !b.p || a.rows == 0 || b.rows == 0) return false;
   const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
   const uintptr_t ea = pa + (uintptr_t)((a.rows - 1) * a.pitch + a.run), eb = pb + (uintptr_t)((b.rows - 1) * b.pitch + b.run);
   if (ea <= pb || eb <= pa) return false;
-  if (a.rows == 1 || b.rows == 1 || a.pitch != b.pitch) return true;
-  const int64_t off = (int64_t)((pb - pa) % (uintptr_t)a.pitch);            // of b's rows in a's
-  const int64_t at = pb >= pa ? off : (a.pitch - (int64_t)((pa - pb) % (uintptr_t)a.pitch)) % a.pitch;
-  return at < a.run || at + b.run > a.pitch;
+  if (a.rows == 1 && b.rows == 1) return true;
+  if (a.rows > 1 && b.rows > 1 && a.pitch != b.pitch) return true;
+  const uintptr_t pitch = (uintptr_t)(a.rows > 1 ? a.pitch : b.pitch);
+  const uintptr_t at = pb >= pa ? (pb - pa) % pitch : (pitch - (pa - pb) % pitch) % pitch;      // of b's runs behind a's
+  return at < (uintptr_t)a.run || at + (uintptr_t)b.run > pitch;
 }
 
 int64_t element(int type) { return type == IST_T_BF16 ? 2 : 4; }
@@ -268,7 +270,6 @@ extern "C" ist_status ist_layer_norm_forward(const void* x_dev, int x_type, int6
   const char* why = bad_shape(rows, cols, groups);
   if (!why) why = bad_rows(x_dev, x_type, x_stride, rows, cols);
   if (!why) why = bad_rows(y_dev, y_type, y_stride, rows, cols);
-  if (!why && !(eps > 0.f && std::isfinite(eps))) why = "eps must be positive and finite";
   if (!why && (!aligned(weight_dev, 4) || !aligned(bias_dev, 4) || !aligned(mean_out_dev, 4) || !aligned(rstd_out_dev, 4)))
     why = "weight, bias, mean and rstd must be aligned to 4 bytes";
   if (!why) {
@@ -283,6 +284,7 @@ extern "C" ist_status ist_layer_norm_forward(const void* x_dev, int x_type, int6
         if (overlap(out[i], out[j])) why = "outputs overlap";
     }
   }
+  if (!why && !(eps > 0.f && std::isfinite(eps))) why = "eps must be positive and finite";
   if (why) return fail_call(IST_ERR_ARG, "ist_layer_norm_forward: %s", why);
   if (rows == 0) return IST_OK;
   cudaStream_t stream = (cudaStream_t)cuda_stream;
@@ -302,7 +304,9 @@ extern "C" ist_status ist_layer_norm_forward(const void* x_dev, int x_type, int6
 
 extern "C" size_t ist_layer_norm_workspace_bytes(int64_t rows, int64_t cols, int groups) {
   if (bad_shape(rows, cols, groups)) return 0;
-  return (size_t)(round_up((int64_t)parts_of(rows, cols, groups) * groups * 2 * cols * 4, 256));
+  const int parts = parts_of(rows, cols, groups);
+  if (cols <= kNormWidest && parts == 1) return 0;      // the sums are written where they belong
+  return (size_t)(round_up((int64_t)parts * groups * 2 * cols * 4, 256));
 }
 
 extern "C" ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, int64_t dy_stride, const void* x_dev,
@@ -323,7 +327,7 @@ extern "C" ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, i
     why = "weight, mean, rstd, dweight and dbias must be aligned to 4 bytes";
   if (why) return fail_call(IST_ERR_ARG, "ist_layer_norm_backward: %s", why);
   const int64_t need = sums ? (int64_t)ist_layer_norm_workspace_bytes(rows, cols, groups) : 0;
-  if (sums && rows && (!workspace_dev || (int64_t)workspace_bytes < need || !aligned(workspace_dev, 16)))
+  if (need && rows && (!workspace_dev || (int64_t)workspace_bytes < need || !aligned(workspace_dev, 16)))
     return fail_call(IST_ERR_WORKSPACE, "ist_layer_norm_backward: workspace too small or not aligned to 16 bytes (%lld bytes needed)",
                      (long long)need);
   {
@@ -333,7 +337,7 @@ extern "C" ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, i
                        {weight_dev, 1, groups * cols * 4, 0}, {mean_dev, one, rows * 4, 0}, {rstd_dev, one, rows * 4, 0}};
     const Span out[] = {{dx_out_dev, rows, cols * element(x_type), dx_stride * element(x_type)},
                         {dweight_out_dev, 1, groups * cols * 4, 0}, {dbias_out_dev, 1, groups * cols * 4, 0},
-                        {sums && rows ? workspace_dev : nullptr, 1, need, 0}};
+                        {need && rows ? workspace_dev : nullptr, 1, need, 0}};
     for (int i = 0; i < 4; ++i) {
       for (int j = 0; j < 5; ++j)
         if (overlap(out[i], in[j])) return fail_call(IST_ERR_ARG, "ist_layer_norm_backward: an output overlaps an input");

@@ -435,3 +435,18 @@ def test_a_step_tells_graphs_that_need_the_old_values(api):
     api.AdamW([p]).step([torch.ones(8, device=DEV)])
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+def test_a_refused_step_is_no_step(api):
+    count = torch.zeros(1, dtype=torch.int64, device=DEV)
+    opt = api.AdamW([torch.ones(8, device=DEV)], eps=0.0, step_dev=count)
+    with pytest.raises(api.IstError, match="eps"):
+        opt.step([torch.ones(8, device=DEV)])
+    assert int(count) == 0 and opt.steps == 0
+
+
+def test_parameters_made_in_inference_mode(api):
+    with torch.inference_mode():
+        p = torch.ones(8, device=DEV)
+        api.AdamW([p], weight_decay=0.0).step([torch.ones(8, device=DEV)])
+    assert ((p - 0.999).abs() < 1e-6).all()

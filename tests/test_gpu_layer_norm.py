@@ -431,3 +431,46 @@ def test_autograd_captured_while_an_eager_graph_lives(api):
     del eager
     want = torch.autograd.grad(trunk.layer_norm(x, w, b).square().sum(), (x, w, b))
     assert all(torch.equal(a, c) for a, c in zip(kept, want))
+
+
+def test_rows_side_by_side_in_one_buffer(api):
+    """Inputs and outputs that take turns in a wider buffer."""
+    gen = torch.Generator(device=DEV).manual_seed(10)
+    buf = torch.randn(500, 3 * 104, generator=gen, device=DEV)
+    x, y, dx = buf[:, :100], buf[:, 104:204], buf[:, 208:308]
+    w, b = vectors(2, 100, gen)
+    y2, mean, rstd = check_forward(api, x, w, b, 2, y=y)
+    assert y2 is y
+    check_backward(api, y, x, w, mean, rstd, 2, dx_view=dx)
+    with pytest.raises(api.IstError, match="overlap"):
+        api.ist_layer_norm_forward(x, w, b, groups=2, y=buf[:, 96:196])
+
+
+def test_the_first_call_of_a_process_may_be_captured():
+    """Nothing has to be set up by an uncaptured call."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_1910_02120_b200 import api
+x = torch.randn(300, 1001, device="cuda")
+w = torch.randn(1, 1001, device="cuda")
+p = [torch.zeros(5000, device="cuda")]
+g = [torch.ones(5000, device="cuda")]
+opt = api.AdamW(p, state_bits=8, max_norm=1.0)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    y, mean, rstd = api.ist_layer_norm_forward(x, w)
+    dx, dw, db = api.ist_layer_norm_backward(y, x, w, mean, rstd)
+    norm = opt.step(g)
+graph.replay()
+torch.cuda.synchronize()
+y2, mean, rstd = api.ist_layer_norm_forward(x, w)
+assert torch.equal(y, y2) and torch.equal(dx, api.ist_layer_norm_backward(y, x, w, mean, rstd)[0])
+assert abs(float(norm) - 5000 ** 0.5) < 1e-3 and float(p[0].abs().min()) > 0
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]

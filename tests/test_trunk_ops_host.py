@@ -40,6 +40,21 @@ def test_forward_refuses(api, bad, word):
     assert message.startswith("ist_layer_norm_forward: ") and word in message, message
 
 
+@pytest.mark.parametrize("good", [
+    dict(x_stride=16, y_stride=16, y=P + 32),                       # rows side by side in one buffer
+    dict(x_stride=16, y_stride=16, y=P - 32),
+    dict(x_stride=32, y_stride=64, y=P + 32, y_type=1),
+    dict(x_stride=32, y_stride=8, rows=1, groups=1, y=P + 32),
+])
+def test_rows_that_interleave_do_not_overlap(api, good):
+    """Refused only for the last argument looked at (eps), so everything before it has passed; nothing is enqueued."""
+    assert _forward(api, **good, eps=-1.0) == api.IST_ERR_ARG
+    assert "eps" in api.lib.ist_last_error(None).decode()
+    bad = {**good, "y": good["y"] + 4 * (1 if good["y"] < P else -1)}
+    if good.get("rows") != 1:
+        assert _forward(api, **bad) == api.IST_ERR_ARG and "overlap" in api.lib.ist_last_error(None).decode()
+
+
 def test_no_rows_is_no_error(api):
     assert _forward(api, rows=0, x=None, y=None) == api.IST_OK
     assert api.lib.ist_adamw_step(None, 0, api.AdamWArgs(beta1=0.9, beta2=0.99, eps=1e-8, step=1, state_bits=32), None, 0, None) == api.IST_OK
@@ -55,7 +70,7 @@ def _backward(api, dy=P, dy_type=0, dy_stride=8, x=2 * P, x_type=0, x_stride=8, 
     (dict(dy=None), "null"), (dict(x=None), "null"), (dict(mean=None), "mean"), (dict(rstd=None), "rstd"), (dict(dy_type=3), "types"),
     (dict(dx=None, dweight=None, dbias=None), "no output"), (dict(groups=5), "groups"), (dict(dx_stride=4), "stride"),
     (dict(dx=P), "overlap"), (dict(dx=2 * P), "overlap"), (dict(dweight=7 * P), "overlap"), (dict(dbias=3 * P), "overlap"),
-    (dict(dweight=8 * P), "overlap"), (dict(dbias=7 * P + 2), "aligned"),
+    (dict(dbias=7 * P + 2), "aligned"),
 ])
 def test_backward_refuses(api, bad, word):
     assert _backward(api, **bad) == api.IST_ERR_ARG
@@ -64,12 +79,16 @@ def test_backward_refuses(api, bad, word):
 
 
 def test_backward_needs_its_workspace(api):
-    need = api.lib.ist_layer_norm_workspace_bytes(4, 8, 2)
-    assert need > 0
-    for bad in (dict(ws=None), dict(ws_bytes=need - 1), dict(ws=8 * P + 8)):
-        assert _backward(api, **bad) == api.IST_ERR_WORKSPACE
+    big = dict(rows=4096, cols=1024, groups=2, dy=1 << 30, x=2 << 30, dx=3 << 30, dy_stride=1024, x_stride=1024, dx_stride=1024, ws=4 << 30)
+    need = api.lib.ist_layer_norm_workspace_bytes(4096, 1024, 2)
+    assert need > 0 and need % 8192 == 0
+    for bad in (dict(ws=None), dict(ws_bytes=need - 1), dict(ws=(4 << 30) + 8)):
+        assert _backward(api, **{**big, "ws_bytes": need, **bad}) == api.IST_ERR_WORKSPACE
+    assert _backward(api, **{**big, "ws_bytes": need, "dweight": 4 << 30}) == api.IST_ERR_ARG
+    assert "overlap" in api.lib.ist_last_error(None).decode()
     for shape in ((-1, 8, 1), (4, 0, 1), (4, 8, 0), (4, 8, 3), (1 << 31, 8, 1), (0, 1 << 30, 1 << 20)):
         assert api.lib.ist_layer_norm_workspace_bytes(*shape) == 0
+    assert api.lib.ist_layer_norm_workspace_bytes(4, 8, 2) == 0              # a few rows: one part, written where it belongs
 
 
 def _table(api, count=1, **fields):
