@@ -283,8 +283,8 @@ bool dispatch(const NormBackward& a, cudaStream_t stream, cudaError_t* e) {
   } else {
     TAKE(0, 1, 4, 8, 4, 3, 1);
     TAKE(33, 1, 8, 8, 2, 3, 1);
-    TAKE(65, 1, 8, 16, 2, 3, 1);
-    TAKE(129, 1, 8, 32, 2, 3, 1);
+    TAKE(65, 1, S == 4 ? 16 : 8, S == 4 ? 8 : 16, S == 4 ? 1 : 2, 3, 1);
+    TAKE(129, 1, S == 4 ? 16 : 8, S == 4 ? 16 : 32, S == 4 ? 1 : 2, 3, 1);
     TAKE(257, 1, 16, 32, R, D, 1);
     TAKE(513, 1, 16, 64, R, D, 1);
     TAKE(1025, 1, 16, 128, R, D, 1);

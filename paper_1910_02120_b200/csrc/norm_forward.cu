@@ -272,12 +272,12 @@ bool dispatch(const NormForward& a, cudaStream_t stream, cudaError_t* e) {
   } else {
     TAKE(0, 1, 4, 8, 4, 3, 1);
     TAKE(33, 1, 8, 8, 4, 3, 1);
-    TAKE(65, 1, 8, 16, 4, 3, 1);
-    TAKE(129, 1, 8, 32, 4, 3, 1);
+    TAKE(65, 1, 16, 8, 2, 3, 1);
+    TAKE(129, 1, 16, 16, 2, 3, 1);
     TAKE(257, 1, 12, 32, 1, 4, 1);
     TAKE(385, 1, 16, 32, 1, 4, 1);
-    TAKE(513, 1, 12, 64, 1, 4, 1);
-    TAKE(769, 1, 16, 64, 1, 4, 1);
+    TAKE(513, 1, 24, 32, 1, 3, 1);
+    TAKE(769, 1, 32, 32, 1, 3, 1);
     TAKE(1025, 1, 12, 128, 1, 4, 1);
     TAKE(1537, 1, 16, 128, 1, 4, 1);
     TAKE(2049, 1, 16, 256, 2, 3, 1);
