@@ -8,7 +8,7 @@ namespace ist {
 namespace {
 
 // 51,200 bf16 rows of 1024: 36.7 us, 0.88 of the copy rate; 4096 fp32 rows of 16384 to bf16: 71 us, 0.87.  9600 fp32 rows of 1001,
-// which start anywhere: 15.6 us, against 11.5 us for 1000 columns.
+// which start anywhere: 14.1 us, against 11.5 us for 1000 columns.
 template <typename XT, typename YT, int V, int NV, int TPR, int RB, int D, int CL, int LEAST>
 __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_forward_kernel(const NormForward a) {
   constexpr int kThreads = TPR > kNormThreads ? TPR : kNormThreads, kSlots = kThreads / TPR, kTile = kSlots * RB;
@@ -248,8 +248,9 @@ bool dispatch(const NormForward& a, cudaStream_t stream, cudaError_t* e) {
   auto fits = [&](const void* p, int64_t ld, int size) { return (((uintptr_t)p | (uintptr_t)(ld * size)) & (V * size - 1)) == 0; };
   const bool pieces = a.cols % V == 0 && fits(a.x, a.x_ld, sizeof(XT)) && fits(a.y, a.y_ld, sizeof(YT));
   const int n = a.cols;
-  // Eight columns a thread keep a warp at a row or less up to 256, sixteen a block of 256 up to 4096; two and four rows at a
-  // time then take the place of more columns.  A row of 16384 goes to one block with 32 columns a thread (35 us for 134 MB read and 67
+  // Eight or sixteen columns a thread up to 4096 and two or four rows at a time, so that what a row costs is shared by 32 elements of a
+  // thread; rows that start anywhere cost more, and a warp alone takes one of up to 1024 (bf16 rows of 1001: 34.9 us, 44.8 us with 64
+  // threads a row and a barrier between them).  A row of 16384 goes to one block with 32 columns a thread (35 us for 134 MB read and 67
   // written): two blocks of 16 columns a thread exchange sums twice a row and took 57 us.
   // least: columns that are too many for the line before; of a cluster's block, which may have as little as none, 0
 #define TAKE(least, v, nv, tpr, rb, d, cl)                                                                  \

@@ -474,3 +474,21 @@ assert abs(float(norm) - 5000 ** 0.5) < 1e-3 and float(p[0].abs().min()) > 0
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
     assert done.returncode == 0, done.stderr[-2000:]
+
+
+def test_autograd_of_sites_into_bf16(api):
+    """Every site's weight and bias get their own gradients; the way back starts from a bf16 gradient."""
+    from paper_1910_02120_b200 import trunk
+    gen = torch.Generator(device=DEV).manual_seed(11)
+    x = torch.randn(3 * 50, 136, generator=gen, device=DEV).requires_grad_()
+    w, b = (v.requires_grad_() for v in vectors(3, 136, gen))
+    y = trunk.layer_norm(x, w, b, groups=3, y_dtype=BF16)
+    dy = torch.randn(150, 136, generator=gen, device=DEV).to(BF16)
+    assert y.dtype == BF16
+    y.backward(dy)
+    x64, w64, b64 = (v.detach().double().requires_grad_() for v in (x, w, b))
+    h = ((x64 - x64.mean(-1, keepdim=True)) / (x64.var(-1, correction=0, keepdim=True) + 1e-5).sqrt()).view(3, 50, 136)
+    (h * w64[:, None] + b64[:, None]).view(150, 136).backward(dy.double())
+    for a, c in ((x, x64), (w, w64), (b, b64)):
+        assert a.grad.shape == a.shape
+        assert ((a.grad.double() - c.grad).abs() <= 256 * U * (c.grad.abs() + c.grad.abs().max())).all()
