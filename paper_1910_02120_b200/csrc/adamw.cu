@@ -195,24 +195,55 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     const bool vec = e.index & kAligned;
     float* const em = (float*)e.m;
     float* const ev = (float*)e.v;
+    if (vec) {
 #pragma unroll
-    for (int u = 0; u < kChunk / (4 * kThreads); ++u) {
-      const int64_t i = first + (u * kThreads + threadIdx.x) * 4;
-      if (i >= e.n) break;
-      float p[4], g[4], m[4], v[4];
-      get4(e.p, i, e.n, vec, p);
-      get4((const GT*)e.g, i, e.n, vec, g);
-      get4(em, i, e.n, vec, m);
-      get4(ev, i, e.n, vec, v);
+      for (int u = 0; u < kChunk / (4 * kThreads); ++u) {
+        const int64_t i = first + (u * kThreads + threadIdx.x) * 4;
+        if (i >= e.n) break;
+        float p[4], g[4], m[4], v[4];
+        get4(e.p, i, e.n, true, p);
+        get4((const GT*)e.g, i, e.n, true, g);
+        get4(em, i, e.n, true, m);
+        get4(ev, i, e.n, true, v);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        moments(a, s.clip, g[k], &m[k], &v[k]);
-        p[k] = update(a, s, e.decay, p[k], m[k], v[k]);
+        for (int k = 0; k < 4; ++k) {
+          moments(a, s.clip, g[k], &m[k], &v[k]);
+          p[k] = update(a, s, e.decay, p[k], m[k], v[k]);
+        }
+        put4(e.p, i, e.n, true, p);
+        put4(em, i, e.n, true, m);
+        put4(ev, i, e.n, true, v);
+        if (e.copy) put4(e.copy, i, e.n, true, p);
       }
-      put4(e.p, i, e.n, vec, p);
-      put4(em, i, e.n, vec, m);
-      put4(ev, i, e.n, vec, v);
-      if (e.copy) put4(e.copy, i, e.n, vec, p);
+    } else {
+      // arrays that start anywhere: adjacent threads take adjacent values
+#pragma unroll
+      for (int u = 0; u < kChunk / (4 * kThreads); ++u) {
+        const int64_t i = first + u * (4 * kThreads) + threadIdx.x;
+        float p[4], g[4], m[4], v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int64_t at = i + k * kThreads;
+          if (at < e.n) {
+            p[k] = e.p[at];
+            g[k] = to_float(((const GT*)e.g)[at]);
+            m[k] = em[at];
+            v[k] = ev[at];
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int64_t at = i + k * kThreads;
+          if (at < e.n) {
+            moments(a, s.clip, g[k], &m[k], &v[k]);
+            p[k] = update(a, s, e.decay, p[k], m[k], v[k]);
+            e.p[at] = p[k];
+            em[at] = m[k];
+            ev[at] = v[k];
+            if (e.copy) e.copy[at] = from_float<bf16>(p[k]);
+          }
+        }
+      }
     }
   }
 }
@@ -468,10 +499,20 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const __grid_consta
     const bool vec = ((uintptr_t)e.g & (4 * sizeof(GT) - 1)) == 0;
 #pragma unroll 1
     for (int at = 0; at < chunk; at += kChunk) {
-      const int64_t first = (int64_t)(c - t.chunk0[j]) * chunk + at + threadIdx.x * 4, past = min(e.n, (int64_t)(c - t.chunk0[j] + 1) * chunk);
+      const int64_t first = (int64_t)(c - t.chunk0[j]) * chunk + at, past = min(e.n, (int64_t)(c - t.chunk0[j] + 1) * chunk);
       float g[U][4];
+      if (vec) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) get4((const GT*)e.g, first + u * kThreads * 4, past, vec, g[u]);
+        for (int u = 0; u < U; ++u) get4((const GT*)e.g, first + (u * kThreads + threadIdx.x) * 4, past, true, g[u]);
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int64_t i = first + (u * 4 + k) * kThreads + threadIdx.x;
+            g[u][k] = i < past ? to_float(((const GT*)e.g)[i]) : 0.f;
+          }
+      }
       float q = 0.f;
 #pragma unroll
       for (int u = 0; u < U; ++u)
