@@ -385,6 +385,8 @@ enum { IST_T_F32 = 0, IST_T_BF16 = 1 };
  * fp32 (differences of up to about 1e18 in a row of a million elements).  rows = 0 is allowed.  0 < eps < inf.
  * 1 <= cols <= 2^30, 0 <= rows <= 2^31 - 65536, 1 <= groups < 2^31.  Outputs must not overlap inputs or one another
  * (rows of one buffer that interleave without sharing elements are fine).  Elements between the rows are left as they are.
+ * Very wide rows are shared by several blocks, whose waits for one another are bounded (about a second): rows of a wait that gave
+ * up come out as NaN.
  */
 ist_status ist_layer_norm_forward(const void* x_dev, int x_type, int64_t x_stride, int64_t rows, int64_t cols,
                                   int groups, const float* weight_dev, const float* bias_dev, float eps, void* y_dev,
