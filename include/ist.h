@@ -398,7 +398,7 @@ ist_status ist_layer_norm_forward(const void* x_dev, int x_type, int64_t x_strid
  *   dx_j = rstd * (g_j - sum_i g_i / cols - h_j * sum_i g_i h_i / cols)   (x's type),
  *   dweight = sum over the site's rows of dy * h,   dbias = sum over the site's rows of dy   ([groups][cols] fp32).
  * dx_out_dev, dweight_out_dev and dbias_out_dev may be NULL where they are not wanted (not all three).  The sums over rows
- * are added in an order that depends on the shape alone, so results are the same from call to call.  rows = 0 gives
+ * are added in an order that depends on shape, types and alignment alone, so results are the same from call to call.  rows = 0 gives
  * zeros for dweight and dbias.  workspace_dev: at least ist_layer_norm_workspace_bytes(rows, cols, groups) bytes
  * (0 where none is needed, and on invalid arguments, which the call then refuses), 16-byte aligned; may be NULL where none is needed or neither
  * dweight nor dbias is wanted; its content means nothing before and after the call.
