@@ -580,7 +580,10 @@ class AdamW:
     weight_decay: a number, or one per tensor.  max_norm: bound of the global gradient norm (None: no clipping).
     step: steps taken so far.  step_dev (int64 [1]), lr_dev (fp32 [1]): device scalars that replace the host's step and lr,
     for steps that are captured into a graph; step() then adds one to step_dev on the stream before the update.
-    A step runs on `stream` or on the device's current stream."""
+    A step runs on `stream` or on the device's current stream.  With `stream` the object's own states and workspace belong to that
+    stream from the start; without it, to the stream that is current at construction, and steps on another one have to be ordered
+    behind it.  What the caller hands in (parameters, copies, states, gradients) the caller orders before a step's stream.  The
+    object has to outlive the graphs that captured its steps."""
 
     def __init__(self, params: Sequence[torch.Tensor], lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999),
                  eps: float = 1e-8, weight_decay=0.01, state_bits: int = 32, max_norm: Optional[float] = None,
@@ -608,7 +611,8 @@ class AdamW:
         shapes = {n: (torch.int16, total // IST_ADAMW_BLOCK) if n.endswith("base") else
                   (torch.uint8 if state_bits == 8 else torch.float32, total) for n in names}
         if state is None:
-            state = {n: torch.zeros(size, dtype=dtype, device=dev) for n, (dtype, size) in shapes.items()}
+            with torch.cuda.stream(stream):             # the steps' stream: its first reads come after these writes
+                state = {n: torch.zeros(size, dtype=dtype, device=dev) for n, (dtype, size) in shapes.items()}
         if set(state) != set(names):
             _refuse(f"state needs {names}")
         for n, (dtype, size) in shapes.items():
@@ -648,7 +652,8 @@ class AdamW:
         self.workspace = None
         self.workspace_bytes = int(lib.ist_adamw_workspace_bytes(len(self.params))) if max_norm else 0
         if max_norm:
-            self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
+            with torch.cuda.stream(stream):
+                self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
 
     def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, lr: Optional[float] = None) -> Optional[torch.Tensor]:
         """One step with `grads` (default: the parameters' .grad), all fp32 or all bf16; a None passes its tensor over.
