@@ -571,12 +571,20 @@ def ist_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[
     return dx, dweight, dbias
 
 
+def _cuda_device(t: torch.Tensor, name: str) -> torch.device:
+    if t.device.type != "cuda":
+        _refuse(f"{name} are on {t.device}: a CUDA device is needed")
+    return t.device
+
+
 class AdamW:
     """AdamW over a list of fp32 tensors, one ist_adamw_step per step(): borrows the parameters (and their bf16 operand
     `copies`, where given) and owns the states, unless they are handed in.
 
     state: {"exp_avg", "exp_avg_sq"} and with state_bits = 8 {"exp_avg_base", "exp_avg_sq_base"}: flat tensors in which
     tensor i starts at offsets[i], a multiple of IST_ADAMW_BLOCK values; zeros before the first step.
+    A step looks where its tensors lie: parameters, copies and entries of `state` may be given other storage of the same size
+    and type (Module.to and back, `p.data = ...`, a loaded state) between steps; a captured step keeps the storage of its capture.
     weight_decay: a number, or one per tensor.  max_norm: bound of the global gradient norm (None: no clipping).
     step: steps taken so far.  step_dev (int64 [1]), lr_dev (fp32 [1]): device scalars that replace the host's step and lr,
     for steps that are captured into a graph; step() then adds one to step_dev on the stream before the update.
@@ -593,12 +601,11 @@ class AdamW:
         self.params, self.copies = list(params), None if copies is None else list(copies)
         if not self.params:
             _refuse("no parameters")
-        self.device = dev = self.params[0].device
-        if dev.type != "cuda":
-            _refuse(f"parameters are on {dev}: a CUDA device is needed")
+        dev = self.device = _cuda_device(self.params[0], "parameters")
+        self.index = self.params[0].get_device()
         if state_bits not in (8, 32):
             _refuse("state_bits is 32 or 8")
-        self.lr, self.steps, self.stream, self.index = float(lr), int(step), stream, dev.index
+        self.lr, self.steps, self.stream = float(lr), int(step), stream
         if stream is not None and stream.device != dev:
             _refuse(f"the stream belongs to another device than {dev}")
         self.sizes = [p.numel() for p in self.params]
@@ -608,52 +615,73 @@ class AdamW:
             self.offsets.append(self.offsets[-1] + r)
         total = self.offsets.pop()
         names = ["exp_avg", "exp_avg_sq"] + (["exp_avg_base", "exp_avg_sq_base"] if state_bits == 8 else [])
-        shapes = {n: (torch.int16, total // IST_ADAMW_BLOCK) if n.endswith("base") else
-                  (torch.uint8 if state_bits == 8 else torch.float32, total) for n in names}
+        self.shapes = {n: (torch.int16, total // IST_ADAMW_BLOCK) if n.endswith("base") else
+                       (torch.uint8 if state_bits == 8 else torch.float32, total) for n in names}
         if state is None:
             with torch.cuda.stream(stream):             # the steps' stream: its first reads come after these writes
-                state = {n: torch.zeros(size, dtype=dtype, device=dev) for n, (dtype, size) in shapes.items()}
-        if set(state) != set(names):
-            _refuse(f"state needs {names}")
-        for n, (dtype, size) in shapes.items():
-            t = state[n]
-            if t.device != dev or t.dtype != dtype or tuple(t.shape) != (size,) or not t.is_contiguous():
-                _refuse(f"state {n} must be {size} contiguous values of {dtype} on {dev}")
+                state = {n: torch.zeros(size, dtype=dtype, device=dev) for n, (dtype, size) in self.shapes.items()}
         self.state = dict(state)
-        if self.copies is not None and len(self.copies) != len(self.params):
-            _refuse("one copy per parameter is needed")
-        for name, tensors, dtype in (("parameter", self.params, torch.float32), ("copy", self.copies or [], torch.bfloat16)):
-            for i, t in enumerate(tensors):
-                if t.device != dev or t.dtype != dtype or t.numel() != self.sizes[i] or not t.is_contiguous():
-                    _refuse(f"{name} {i} must be {self.sizes[i]} contiguous values of {dtype} on {dev}")
-        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
-                       for t in self.params + (self.copies or []) + list(self.state.values()) if t.numel())
-        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
-            _refuse("parameters, copies and states must not overlap")
         decay = [float(weight_decay)] * len(self.params) if isinstance(weight_decay, (int, float)) else [float(d) for d in weight_decay]
         if len(decay) != len(self.params):
             _refuse("one weight decay per parameter is needed")
         self.table = np.zeros(len(self.params), ADAMW_TENSOR)
-        self.table["param"] = [p.data_ptr() for p in self.params]
-        for n in names:
-            base, size, per = self.state[n].data_ptr(), self.state[n].element_size(), IST_ADAMW_BLOCK if n.endswith("base") else 1
-            self.table[n] = [base + o // per * size for o in self.offsets]
-        if self.copies is not None:
-            self.table["param_bf16"] = [c.data_ptr() for c in self.copies]
         self.table["n"], self.table["weight_decay"] = self.sizes, decay
-        for name, t, dtype in (("step_dev", step_dev, torch.int64), ("lr_dev", lr_dev, torch.float32)):
-            if t is not None and (t.device != dev or t.dtype != dtype or t.numel() != 1):
-                _refuse(f"{name} must be one value of {dtype} on {dev}")
-        self.step_dev, self.lr_dev = step_dev, lr_dev
         self.table_at, self.words = self.table.ctypes.data, memoryview(self.table.view(np.uint64)).cast("B").cast("Q")
+        self.step_dev, self.lr_dev = step_dev, lr_dev
         self.args = AdamWArgs(lr=self.lr, beta1=betas[0], beta2=betas[1], eps=eps, max_norm=max_norm or 0.0,
-                              seed=seed & (2 ** 64 - 1), state_bits=state_bits, step_dev=_ptr(step_dev), lr_dev=_ptr(lr_dev))
-        self.written = [t for t in self.params + (self.copies or []) if not t.is_inference()]
+                              seed=seed & (2 ** 64 - 1), state_bits=state_bits)
+        self._bind()
         self.workspace = None
         self.workspace_bytes = int(lib.ist_adamw_workspace_bytes(len(self.params))) if max_norm else 0
         if max_norm:
             with torch.cuda.stream(stream):
                 self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
+                self.norm_like = torch.empty(1, dtype=torch.float32, device=dev)
+
+    def _tensors(self) -> List[torch.Tensor]:
+        """Everything whose address a step hands to the library, but for the gradients."""
+        tensors = [*self.params, *self.state.values()]
+        if self.copies is not None:
+            tensors += self.copies
+        if self.step_dev is not None:
+            tensors.append(self.step_dev)
+        if self.lr_dev is not None:
+            tensors.append(self.lr_dev)
+        return tensors
+
+    def _bind(self) -> None:
+        """Checks the tensors and notes where they lie."""
+        dev, params, copies, state = self.device, self.params, self.copies, self.state
+        if set(state) != set(self.shapes):
+            _refuse(f"state needs {list(self.shapes)}")
+        for n, (dtype, size) in self.shapes.items():
+            t = state[n]
+            if t.device != dev or t.dtype != dtype or tuple(t.shape) != (size,) or not t.is_contiguous():
+                _refuse(f"state {n} must be {size} contiguous values of {dtype} on {dev}")
+        if len(params) != len(self.sizes):
+            _refuse(f"{len(params)} parameters, not {len(self.sizes)}")
+        if copies is not None and len(copies) != len(params):
+            _refuse("one copy per parameter is needed")
+        for name, tensors, dtype in (("parameter", params, torch.float32), ("copy", copies or [], torch.bfloat16)):
+            for i, t in enumerate(tensors):
+                if t.device != dev or t.dtype != dtype or t.numel() != self.sizes[i] or not t.is_contiguous():
+                    _refuse(f"{name} {i} must be {self.sizes[i]} contiguous values of {dtype} on {dev}")
+        for name, t, dtype in (("step_dev", self.step_dev, torch.int64), ("lr_dev", self.lr_dev, torch.float32)):
+            if t is not None and (t.device != dev or t.dtype != dtype or t.numel() != 1):
+                _refuse(f"{name} must be one value of {dtype} on {dev}")
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+                       for t in params + (copies or []) + list(state.values()) if t.numel())
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            _refuse("parameters, copies and states must not overlap")
+        self.table["param"] = [p.data_ptr() for p in params]
+        for n in self.shapes:
+            base, size, per = state[n].data_ptr(), state[n].element_size(), IST_ADAMW_BLOCK if n.endswith("base") else 1
+            self.table[n] = [base + o // per * size for o in self.offsets]
+        self.table["param_bf16"] = 0 if copies is None else [c.data_ptr() for c in copies]
+        self.args.step_dev, self.args.lr_dev = _ptr(self.step_dev), _ptr(self.lr_dev)
+        self.written = [t for t in params + (copies or []) if not t.is_inference()]
+        tensors = self._tensors()
+        self.held = list(map(_Tensor.data_ptr, tensors)), list(map(_Tensor.numel, tensors))
 
     def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, lr: Optional[float] = None) -> Optional[torch.Tensor]:
         """One step with `grads` (default: the parameters' .grad), all fp32 or all bf16; a None passes its tensor over.
@@ -666,14 +694,17 @@ class AdamW:
             grads = [p.grad for p in self.params]
         if len(grads) != len(self.sizes):
             _refuse("one gradient (or None) per parameter is needed")
+        tensors = self._tensors()
+        if list(map(_Tensor.data_ptr, tensors)) != self.held[0] or list(map(_Tensor.numel, tensors)) != self.held[1]:
+            self._bind()
         index, dtype = self.index, None
-        if type(None) in set(map(type, grads)):
+        try:                                            # the table's second word of nine is the gradient's address
+            self.words[1::9] = array("Q", map(_Tensor.data_ptr, grads))
+            given, sizes = grads, self.sizes
+        except TypeError:                               # there is a None among them
             given = [g for g in grads if g is not None]
             sizes = [n for g, n in zip(grads, self.sizes) if g is not None]
             self.words[1::9] = array("Q", [0 if g is None else g.data_ptr() for g in grads])
-        else:                                           # the table's second word of nine is the gradient's address
-            given, sizes = grads, self.sizes
-            self.words[1::9] = array("Q", map(_Tensor.data_ptr, grads))
         if given:
             dtype = given[0].dtype
             if (list(map(_Tensor.numel, given)) != sizes or not all(map(_Tensor.is_contiguous, given))
@@ -690,7 +721,7 @@ class AdamW:
         norm = workspace_at = None
         if self.workspace is not None:
             workspace_at = self.workspace.data_ptr()
-            norm = torch.empty(1, dtype=torch.float32, device=index)
+            norm = torch.empty_like(self.norm_like)     # half the price of an empty() with arguments
             args.norm_out_dev = norm.data_ptr()
         if self.step_dev is not None:
             self.step_dev.add_(1)

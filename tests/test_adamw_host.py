@@ -1,0 +1,72 @@
+"""api.AdamW's host side with a stand-in for the library call: the table that a step hands over has the addresses that its
+tensors have then."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+
+@pytest.fixture
+def api(monkeypatch):
+    from paper_1910_02120_b200 import build
+    build.build()
+    from paper_1910_02120_b200 import api as a
+    monkeypatch.setattr(a, "_cuda_device", lambda t, name: t.device)
+    a.calls = []
+
+    def call(index, function, table_at, count, args, workspace_at, workspace_bytes):
+        rows = np.frombuffer(ctypes.string_at(table_at, count * a.ADAMW_TENSOR.itemsize), a.ADAMW_TENSOR).copy()
+        a.calls.append((rows, args.step_dev, args.lr_dev))
+
+    monkeypatch.setattr(a, "_call", call)
+    yield a
+    del a.calls
+
+
+def check_table(api, opt, bits):
+    rows, step_dev, lr_dev = api.calls[-1]
+    assert [int(r) for r in rows["param"]] == [p.data_ptr() for p in opt.params]
+    assert [int(r) for r in rows["param_bf16"]] == [c.data_ptr() for c in opt.copies]
+    assert list(rows["n"]) == opt.sizes
+    for name in opt.state:
+        per = api.IST_ADAMW_BLOCK if name.endswith("base") else 1
+        assert [int(r) for r in rows[name]] == [opt.state[name][o // per:].data_ptr() for o in opt.offsets], name
+    assert step_dev == opt.step_dev.data_ptr() and lr_dev == opt.lr_dev.data_ptr()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_finds_tensors_whose_storage_changed(api, bits):
+    params, copies = [torch.ones(300), torch.ones(20, 7)], [torch.ones(300).bfloat16(), torch.ones(20, 7).bfloat16()]
+    opt = api.AdamW(params, copies=copies, state_bits=bits, step_dev=torch.zeros(1, dtype=torch.int64), lr_dev=torch.zeros(1))
+    grads = [torch.ones(300), torch.ones(20, 7)]
+    keep = []                                             # so that no address comes back
+    for change in (lambda: None, lambda: setattr(params[1], "data", params[1].data.clone()),
+                   lambda: setattr(copies[0], "data", copies[0].data.clone()),
+                   lambda: params[0].set_(torch.zeros(300)), lambda: opt.params.__setitem__(0, torch.zeros(300)),
+                   lambda: opt.state.__setitem__("exp_avg", opt.state["exp_avg"].clone()),
+                   lambda: setattr(opt, "state", {k: v.clone() for k, v in reversed(opt.state.items())}),
+                   lambda: setattr(opt, "step_dev", torch.zeros(1, dtype=torch.int64)), lambda: setattr(opt, "lr_dev", torch.ones(1))):
+        keep += [t.data for t in opt._tensors()]
+        change()
+        opt.step(grads)
+        check_table(api, opt, bits)
+    assert opt.steps == 9 and len(api.calls) == 9
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_refuses_tensors_that_no_longer_fit(api, bits):
+    for change in (lambda o: setattr(o.params[0], "data", o.params[0].data[:200]),                 # the same address
+                   lambda o: setattr(o.params[0], "data", o.params[0].data.double()),
+                   lambda o: setattr(o.params[0], "data", torch.zeros(600)[::2]),
+                   lambda o: setattr(o.copies[1], "data", o.params[1].data), lambda o: o.copies.pop(), lambda o: o.params.pop(),
+                   lambda o: setattr(o.params[1], "data", o.params[0].data[100:]),                 # overlaps
+                   lambda o: o.state.__setitem__("exp_avg", o.state["exp_avg"][:256]), lambda o: o.state.pop("exp_avg"),
+                   lambda o: setattr(o, "lr_dev", torch.zeros(2))):
+        params = [torch.ones(300), torch.ones(200)]
+        opt = api.AdamW(params, copies=[p.bfloat16() for p in params], state_bits=bits, lr_dev=torch.zeros(1))
+        change(opt)
+        for _ in range(2):
+            with pytest.raises(api.IstError):
+                opt.step([torch.ones(300), torch.ones(200)])
+        assert opt.steps == 0 and not api.calls

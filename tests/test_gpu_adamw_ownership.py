@@ -33,3 +33,48 @@ def test_states_are_made_on_the_stream_of_the_steps(api, bits):
     assert torch.equal(p, want_p) and torch.equal(norm, want_norm)
     assert all(torch.equal(opt.state[k], want.state[k]) for k in want.state)
     assert all(torch.equal(a, b) for a, b in zip(values, want_values))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_follows_tensors_whose_storage_changed(api, bits):
+    """Parameters taken to the host and back, a copy and a state given other storage: the steps go on as if nothing had moved."""
+    runs = []
+    for moves in (False, True):
+        gen = torch.Generator(device=DEV).manual_seed(2)
+        layer = torch.nn.Linear(300, 77).to(DEV)
+        with torch.no_grad():
+            for p in layer.parameters():
+                p.copy_(torch.randn(p.shape, generator=gen, device=DEV))
+        params = list(layer.parameters())
+        copies = [torch.zeros(p.shape, dtype=torch.bfloat16, device=DEV) for p in params]
+        opt = api.AdamW(params, copies=copies, state_bits=bits, max_norm=1.0, seed=5)
+        keep = []
+        for t in range(4):
+            if moves and t:
+                keep += [p.data for p in params] + list(opt.state.values()) + [c.data for c in copies]    # no address comes back
+                layer.cpu()
+                layer.cuda()
+                copies[t % 2].data = copies[t % 2].data.clone()
+                opt.state["exp_avg"] = opt.state["exp_avg"].clone()
+                stale = [k.clone() for k in keep]
+            opt.step([torch.randn(p.shape, generator=gen, device=DEV) for p in params])
+            if moves and t:
+                now = {x.data_ptr() for x in opt._tensors()}
+                assert all(torch.equal(a, b) for a, b in zip(keep, stale) if a.data_ptr() not in now)
+        runs.append([p.data for p in params] + copies + list(opt.state_values()))
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+def test_a_captured_step_finds_what_was_moved_before_the_capture(api):
+    p = torch.nn.Parameter(torch.ones(5000, device=DEV))
+    g = torch.ones(5000, device=DEV)
+    opt = api.AdamW([p], lr=0.1, weight_decay=0.0)
+    opt.step([g])
+    first = p.data
+    p.data = p.data.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step([g])
+    graph.replay()
+    torch.cuda.synchronize()
+    assert ((first - 0.9).abs() < 1e-5).all() and ((p.data - 0.8).abs() < 1e-5).all()
