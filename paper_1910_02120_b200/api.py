@@ -715,9 +715,8 @@ class AdamW:
             raise TypeError(f"unsupported gradient dtype {dtype}")
         args = self.args
         args.grad_type = kind
-        if lr is not None:
-            self.lr = float(lr)
-        args.lr, args.step = self.lr, self.steps + 1
+        rate = self.lr if lr is None else float(lr)
+        args.lr, args.step = rate, self.steps + 1
         norm = workspace_at = None
         if self.workspace is not None:
             workspace_at = self.workspace.data_ptr()
@@ -732,6 +731,7 @@ class AdamW:
                 self.step_dev.sub_(1)
             raise
         self.steps += 1
+        self.lr = rate
         torch.autograd.graph.increment_version(self.written)    # a graph that still needs the old values is told
         return norm
 

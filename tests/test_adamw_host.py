@@ -70,3 +70,20 @@ def test_a_step_refuses_tensors_that_no_longer_fit(api, bits):
             with pytest.raises(api.IstError):
                 opt.step([torch.ones(300), torch.ones(200)])
         assert opt.steps == 0 and not api.calls
+
+
+def test_a_refused_step_keeps_the_rate(api, monkeypatch):
+    opt = api.AdamW([torch.ones(8)], lr=0.25)
+    accepted = api._call
+
+    def refuse(index, function, table_at, count, args, *rest):
+        if args.lr != 0.125:
+            raise api.IstError(api.IST_ERR_ARG, "lr must be finite")
+        accepted(index, function, table_at, count, args, *rest)
+
+    monkeypatch.setattr(api, "_call", refuse)
+    with pytest.raises(api.IstError):
+        opt.step([torch.ones(8)], lr=float("inf"))
+    assert (opt.lr, opt.steps) == (0.25, 0)
+    opt.step([torch.ones(8)], lr=0.125)
+    assert (opt.lr, opt.steps) == (0.125, 1)
