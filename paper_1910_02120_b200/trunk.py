@@ -5,6 +5,7 @@ from __future__ import annotations
 from typing import Optional
 
 import torch
+from torch.autograd import forward_ad
 
 from . import api
 
@@ -49,7 +50,9 @@ def _check_leaves(tensors) -> None:
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
                groups: int = 1, y_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """Layer norm over the last dimension with gradients for x, weight and bias; see api.ist_layer_norm_forward.
-    A gradient of a gradient is refused."""
+    A gradient of a gradient and forward-mode differentiation are refused."""
+    if forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in (x, weight, bias)):
+        raise api.IstError(api.IST_ERR_UNSUPPORTED, "layer_norm has no forward-mode derivative")
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias)):
         y = _LayerNorm.apply(x, weight, bias, eps, groups, y_dtype)
         _check_leaves((x, weight, bias))          # behind the call: y's graph keeps the leaves' nodes
