@@ -442,6 +442,11 @@ def _call(index: int, function, *args):
         raise IstError(status, lib.ist_last_error(None).decode())
 
 
+def _written(tensors: Sequence[torch.Tensor]) -> None:
+    """Tells autograd of a call's writes: a graph that still needs the old values raises an error when it gets there."""
+    torch.autograd.graph.increment_version([t for t in tensors if not t.is_inference()])
+
+
 def _on(stream: torch.cuda.Stream, tensor: torch.Tensor):
     """Makes `stream` current: what a call allocates then belongs to the stream that it runs on."""
     if stream.device != tensor.device:
@@ -506,7 +511,8 @@ def ist_layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = Non
             return ist_layer_norm_forward(x, weight, bias, eps, groups, y, y_dtype, want_stats)
     cols, index = _norm_shape(x, groups)
     x_type, rows, x_stride = _rows(x, "x", cols, index)
-    if y is None:
+    given = y is not None
+    if not given:
         y = _like(x, y_dtype)
         y_type, y_stride = _TYPES.get(y.dtype, -1), cols
         if y_type < 0:
@@ -523,6 +529,8 @@ def ist_layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = Non
     _call(index, lib.ist_layer_norm_forward, x.data_ptr(), x_type, x_stride, rows, cols, groups,
           _vector(weight, "weight", groups * cols, index), _vector(bias, "bias", groups * cols, index), eps, y.data_ptr(), y_type,
           y_stride, mean_at, rstd_at)
+    if given:
+        _written([y])
     return y, mean, rstd
 
 
@@ -543,8 +551,8 @@ def ist_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[
     cols, index = _norm_shape(x, groups)
     x_type, rows, x_stride = _rows(x, "x", cols, index)
     dy_type, _, dy_stride = _rows(dy, "dy", cols, index, rows)
-    dx_stride = cols
-    if dx is not None:
+    dx_stride, given = cols, dx is not None
+    if given:
         if dx.dtype != x.dtype:
             _refuse("dx must have x's dtype")
         _, _, dx_stride = _rows(dx, "dx", cols, index, rows)
@@ -568,6 +576,8 @@ def ist_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[
     _call(index, lib.ist_layer_norm_backward, dy.data_ptr(), dy_type, dy_stride, x.data_ptr(), x_type, x_stride, rows, cols, groups,
           _vector(weight, "weight", groups * cols, index), _vector(mean, "mean", rows, index),
           _vector(rstd, "rstd", rows, index), dx_at, dx_stride, dweight_at, dbias_at, workspace_at, nbytes)
+    if given:
+        _written([dx])
     return dx, dweight, dbias
 
 
@@ -679,8 +689,8 @@ class AdamW:
             self.table[n] = [base + o // per * size for o in self.offsets]
         self.table["param_bf16"] = 0 if copies is None else [c.data_ptr() for c in copies]
         self.args.step_dev, self.args.lr_dev = _ptr(self.step_dev), _ptr(self.lr_dev)
-        self.written = [t for t in params + (copies or []) if not t.is_inference()]
         tensors = self._tensors()
+        self.written = [t for t in [*params, *(copies or ()), *state.values()] if not t.is_inference()]
         self.held = list(map(_Tensor.data_ptr, tensors)), list(map(_Tensor.numel, tensors))
 
     def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, lr: Optional[float] = None) -> Optional[torch.Tensor]:
