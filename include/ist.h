@@ -363,7 +363,8 @@ const char* ist_last_error(const ist_ctx* ctx);
  * "IST for other architectures": a trunk that every site holds whole).  The paper has no counterpart;
  * ist_local_steps_dx gives such a trunk its gradient, these calls normalise what it hands to the head
  * and update its parameters.  They take no context.  Work is enqueued on cuda_stream (a cudaStream_t,
- * NULL = legacy default stream) of the current device, asynchronously, and may be captured into a
+ * NULL = legacy default stream) of the current device, which may be another one from call to call (launches are sized
+ * for GPUs of one kind), asynchronously, and may be captured into a
  * graph; nothing is allocated and nothing is kept from one call for the next.  Two calls, and two graphs, that may
  * run at the same time need workspaces of their own.  Invalid arguments return an error and enqueue
  * nothing; ist_last_error(NULL) has the message.

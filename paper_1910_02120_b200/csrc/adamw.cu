@@ -3,7 +3,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <mutex>
 #include <type_traits>
 
 #include "kernels.h"
@@ -636,16 +635,15 @@ void fill(const ist_adamw_tensor* list, int64_t count, const ist_adamw_args& a, 
 template <typename GT, int CAP>
 cudaError_t launch8(const Table<CAP>& t, const Args& args, cudaStream_t stream) {
   constexpr int smem = kWarps * kStages * kBlock * (4 + sizeof(GT) + 2);
-  static std::once_flag once;
-  static cudaError_t ready = cudaSuccess;
-  static int resident = 1;
-  std::call_once(once, [] {
-    ready = cudaFuncSetAttribute(adamw8_kernel<GT, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (ready == cudaSuccess) ready = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, adamw8_kernel<GT, CAP>, kThreads, smem);
-    resident = std::max(resident, 1) * sm_count();
+  static OncePerDevice<KernelReady> once;
+  const KernelReady ready = ready_here(once, [] {
+    int per_sm = 1;
+    cudaError_t e = cudaFuncSetAttribute(adamw8_kernel<GT, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, adamw8_kernel<GT, CAP>, kThreads, smem);
+    return KernelReady{e, std::max(per_sm, 1) * sm_count()};
   });
-  if (ready != cudaSuccess) return ready;
-  return launch_pdl(adamw8_kernel<GT, CAP>, dim3((unsigned)std::min(t.chunk0[t.count], resident)), dim3(kThreads), smem, stream, t, args);
+  if (ready.error != cudaSuccess) return ready.error;
+  return launch_pdl(adamw8_kernel<GT, CAP>, dim3((unsigned)std::min(t.chunk0[t.count], ready.resident)), dim3(kThreads), smem, stream, t, args);
 }
 
 template <int CAP>

@@ -2,8 +2,22 @@
 #pragma once
 
 #include "common.cuh"
+#include "per_device.h"
 
 namespace ist {
+
+// Whether a kernel may be launched on a device, and how many of its blocks (or clusters) that device holds.
+struct KernelReady {
+  cudaError_t error;
+  int resident;
+};
+// f(): a KernelReady, worked out once per device; here for the current one.
+template <typename F>
+KernelReady ready_here(OncePerDevice<KernelReady>& once, F f) {
+  int device = 0;
+  const cudaError_t e = cudaGetDevice(&device);
+  return e == cudaSuccess ? once.get(device, f) : KernelReady{e, 0};
+}
 
 struct Launch {
   cudaStream_t stream;

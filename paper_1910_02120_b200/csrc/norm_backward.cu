@@ -1,7 +1,6 @@
 // Layer norm's way back for rows that fit the threads of a block or a cluster: dy and x are read once, dx written, and
 // the sums over rows that dweight and dbias need are kept in registers, a column always with the same thread.
 #include <algorithm>
-#include <mutex>
 
 #include "norm_rows.cuh"
 
@@ -243,10 +242,11 @@ cudaError_t launch(const NormBackward& a, cudaStream_t stream) {
   constexpr int kJoin = kSlots > 1 ? kSlots * 2 * NV * V * TPR * 4 : 0;
   constexpr int kMost = std::max(kJoin, D * kSlots * RB * (row_room(TPR * V * NV, sizeof(XT), V == 1) + row_room(TPR * V * NV, sizeof(DT), V == 1)));
   static_assert(kMost <= 225 * 1024, "ring too large");
-  static std::once_flag once;
-  static cudaError_t ready = cudaSuccess;
-  std::call_once(once, [&] { ready = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost); });
-  if (ready != cudaSuccess) return ready;
+  static OncePerDevice<KernelReady> once;
+  const KernelReady ready = ready_here(once, [&] {
+    return KernelReady{cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost), 0};
+  });
+  if (ready.error != cudaSuccess) return ready.error;
   return launch_rows(kernel, (unsigned)((int64_t)a.sites * a.parts * CL), kThreads, std::max(ring(part_width(a.cols, CL)), kJoin), CL, stream, a);
 }
 

@@ -1,6 +1,5 @@
 // Layer norm's forward pass for rows that fit the threads of a block or a cluster: a row is read once, into registers.
 #include <algorithm>
-#include <mutex>
 
 #include "norm_rows.cuh"
 
@@ -227,17 +226,16 @@ cudaError_t launch(const NormForward& a, cudaStream_t stream) {
   // the most that any width of this instance asks for, and how many blocks an SM holds then
   constexpr int kMost = D * kSlots * RB * row_room(TPR * V * NV, sizeof(XT), V == 1);
   static_assert(kMost <= 225 * 1024, "ring too large");
-  static std::once_flag once;
-  static cudaError_t ready = cudaSuccess;
-  static int resident = 1;
-  std::call_once(once, [&] {
-    ready = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-    if (ready == cudaSuccess) ready = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, kThreads, kMost);
-    resident = std::max(1, (int)(sm_count() * resident / CL));
+  static OncePerDevice<KernelReady> once;
+  const KernelReady ready = ready_here(once, [&] {
+    int per_sm = 1;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kThreads, kMost);
+    return KernelReady{e, std::max(1, sm_count() * per_sm / CL)};
   });
-  if (ready != cudaSuccess) return ready;
+  if (ready.error != cudaSuccess) return ready.error;
   const int64_t tiles = ceil_div(a.site_rows, kSlots * RB) * a.sites;
-  const int64_t blocks = std::min<int64_t>(tiles, resident);
+  const int64_t blocks = std::min<int64_t>(tiles, ready.resident);
   const int smem = D * kSlots * RB * row_room(part_width(a.cols, CL), sizeof(XT), V == 1);
   return launch_rows(kernel, (unsigned)(blocks * CL), kThreads, smem, CL, stream, a);
 }
