@@ -382,8 +382,10 @@ enum { IST_T_F32 = 0, IST_T_BF16 = 1 };
  *   y_j = (x_j - mean) * rstd * weight_j + bias_j.
  * mean_out_dev, rstd_out_dev: [rows] fp32 for the backward pass, either may be NULL.  Statistics are taken
  * in fp32 or wider from the elements' values; y is rounded once, to nearest even.  A row that holds an infinity or
- * a NaN comes out as NaN, other rows are not touched by it.  Squares of a row's differences from its mean have to stay within
- * fp32 (differences of up to about 1e18 in a row of a million elements).  rows = 0 is allowed.  0 < eps < inf.
+ * a NaN comes out as NaN, other rows are not touched by it.  Sums over a row of up to 65,536 columns are fp32 sums and have to
+ * stay within that type's range: the values', and that of the squares of their differences from the mean as it is
+ * rounded.  Magnitudes up to 1e16 are always fine; rows of larger values may come out as NaN or as the bias.
+ * rows = 0 is allowed.  0 < eps < inf.
  * 1 <= cols <= 2^30, 0 <= rows <= 2^31 - 65536, 1 <= groups < 2^31.  Outputs must not overlap inputs or one another
  * (rows of one buffer that interleave without sharing elements are fine).  Elements between the rows are left as they are.
  * Very wide rows are shared by several blocks, whose waits for one another are bounded (about a second): rows of a wait that gave
@@ -399,7 +401,8 @@ ist_status ist_layer_norm_forward(const void* x_dev, int x_type, int64_t x_strid
  *   dx_j = rstd * (g_j - sum_i g_i / cols - h_j * sum_i g_i h_i / cols)   (x's type),
  *   dweight = sum over the site's rows of dy * h,   dbias = sum over the site's rows of dy   ([groups][cols] fp32).
  * dx_out_dev, dweight_out_dev and dbias_out_dev may be NULL where they are not wanted (not all three).  The sums over rows
- * are added in an order that depends on shape, types and alignment alone, so results are the same from call to call.  rows = 0 gives
+ * are added in an order that depends on shape, types, alignment and the number of the GPU's multiprocessors alone, so results are
+ * the same from call to call.  Like those over a row they are fp32 sums and have to stay within that type's range.  rows = 0 gives
  * zeros for dweight and dbias.  workspace_dev: at least ist_layer_norm_workspace_bytes(rows, cols, groups) bytes
  * (0 where none is needed, and on invalid arguments, which the call then refuses), 16-byte aligned; may be NULL where none is needed or neither
  * dweight nor dbias is wanted; its content means nothing before and after the call.
