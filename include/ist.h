@@ -445,7 +445,7 @@ ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, int64_t dy_s
  * norm_out_dev (may be NULL): receives the norm (fp32) if max_norm > 0.
  * workspace_dev: with max_norm > 0 at least ist_adamw_workspace_bytes(count) bytes, 16-byte aligned; else not
  * needed.  Its content means nothing before and after the call.
- * Needs 0 <= beta < 1 for both, eps >= 2^-126, step >= 1, finite lr and weight decays, max_norm >= 0 (infinity: no clipping, but the norm is taken), at most 2^40 values.
+ * Needs 0 <= beta < 1 for both, 2^-126 <= eps <= 2^125, step >= 1, finite lr and weight decays, max_norm >= 0 (infinity: no clipping, but the norm is taken), at most 2^40 values.
  */
 #define IST_ADAMW_BLOCK 128
 typedef struct ist_adamw_tensor {

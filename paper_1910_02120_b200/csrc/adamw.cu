@@ -162,7 +162,7 @@ __device__ __forceinline__ void moments(const Args& a, float clip, float g, floa
   *v = __fadd_rn(__fmul_rn(a.b2, *v), __fmul_rn(__fmul_rn(a.c2, g), g));
 }
 // The root and the reciprocal by the hardware's approximations (2^-23 of their values each; the divisor is a normal number, eps
-// at least, and far from the largest): the change of a parameter is exact to a few units in its last place, and in the
+// at least, and so is its reciprocal): the change of a parameter is exact to a few units in its last place, and in the
 // 8-bit step instructions are what the time goes to.  TINY: eps is so small that roots of denormal numbers weigh beside it.
 template <bool TINY>
 __device__ __forceinline__ float root_of(float v) {
@@ -692,7 +692,8 @@ const char* bad_args(const ist_adamw_args& a) {
   if (a.state_bits != 32 && a.state_bits != 8) return "state_bits is 32 or 8";
   if (a.grad_type != IST_T_F32 && a.grad_type != IST_T_BF16) return "element types are IST_T_F32 and IST_T_BF16";
   if (!(a.beta1 >= 0. && a.beta1 < 1. && a.beta2 >= 0. && a.beta2 < 1.)) return "betas must be in [0, 1)";
-  if (!((float)a.eps >= 1.17549435e-38f && std::isfinite((float)a.eps))) return "eps must be a positive normal number in fp32";
+  // the divisor, eps and a root of 2^91 at most, has a reciprocal that is a normal number too (see inverse)
+  if (!((float)a.eps >= 0x1p-126f && (float)a.eps <= 0x1p125f)) return "eps must be in 2^-126..2^125";
   if (!(a.max_norm >= 0.)) return "max_norm must be >= 0";
   if (!a.lr_dev && !std::isfinite((float)a.lr)) return "lr must be finite";
   if (!a.step_dev && a.step < 1) return "step must be >= 1";

@@ -87,3 +87,13 @@ def test_a_refused_step_keeps_the_rate(api, monkeypatch):
     assert (opt.lr, opt.steps) == (0.25, 0)
     opt.step([torch.ones(8)], lr=0.125)
     assert (opt.lr, opt.steps) == (0.125, 1)
+
+
+@pytest.mark.parametrize("eps, fine", [(2.0 ** -126, True), (2.0 ** 125, True), (2.0 ** 125 * (1 + 2.0 ** -23), False), (1e38, False),
+                                       (2.0 ** -127, False), (float("inf"), False)])
+def test_eps_has_a_reciprocal_in_fp32(api, eps, fine):
+    """The divisor's reciprocal is taken, and is a normal number: one that is flushed to zero would stop the parameters.  A step
+    without tensors enqueues nothing."""
+    args = api.AdamWArgs(lr=1e-3, beta1=0.9, beta2=0.999, eps=eps, step=1, state_bits=32)
+    assert api.lib.ist_adamw_step(None, 0, args, None, 0, None) == (api.IST_OK if fine else api.IST_ERR_ARG)
+    assert fine or "eps" in api.lib.ist_last_error(None).decode()
