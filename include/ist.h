@@ -388,8 +388,8 @@ enum { IST_T_F32 = 0, IST_T_BF16 = 1 };
  * rows = 0 is allowed.  0 < eps < inf.
  * 1 <= cols <= 2^30, 0 <= rows <= 2^31 - 65536, 1 <= groups < 2^31.  Outputs must not overlap inputs or one another
  * (rows of one buffer that interleave without sharing elements are fine).  Elements between the rows are left as they are.
- * Very wide rows are shared by several blocks, whose waits for one another are bounded (about a second): rows of a wait that gave
- * up come out as NaN.
+ * Very wide rows are shared by several blocks, whose waits for one another are bounded (about a second): a wait that gave up
+ * leaves NaN in its row and in those that its block takes after it, and ist_layer_norm_status tells of it.
  */
 ist_status ist_layer_norm_forward(const void* x_dev, int x_type, int64_t x_stride, int64_t rows, int64_t cols,
                                   int groups, const float* weight_dev, const float* bias_dev, float eps, void* y_dev,
@@ -413,6 +413,22 @@ ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, int64_t dy_s
                                    const float* mean_dev, const float* rstd_dev, void* dx_out_dev, int64_t dx_stride,
                                    float* dweight_out_dev, float* dbias_out_dev, void* workspace_dev,
                                    size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Waits for cuda_stream and returns IST_ERR_DEVICE_TIMEOUT if a wait of either pass on the current device gave up since
+ * this was last asked, else IST_OK (IST_ERR_CUDA if the flag cannot be read).  Not for streams under capture.
+ */
+ist_status ist_layer_norm_status(void* cuda_stream);
+
+/*
+ * Self-test of that path (no counterpart in the paper): layer norm of rows x [rows][cols] without weights, fp32, where blocks
+ * withhold their sums from one another, so that the waits for limit_cycles SM clock cycles (1 .. 2e9) must give up.  dy_dev
+ * NULL: the forward pass, out = y.  Else the way back, out = dx, with stats_dev = [rows] means and [rows] reciprocal deviations.
+ * 16385 <= cols <= 65536 (rows that blocks share), 1 <= rows <= 65536.  All of out becomes NaN and ist_layer_norm_status
+ * returns IST_ERR_DEVICE_TIMEOUT; stream and device stay usable.
+ */
+ist_status ist_selftest_layer_norm_wait(const float* x_dev, const float* dy_dev, const float* stats_dev, int64_t rows,
+                                        int64_t cols, float* out_dev, int64_t limit_cycles, void* cuda_stream);
 
 /*
  * One AdamW step over many tensors.  For every parameter, with gradient g, step number t (1 for the first) and

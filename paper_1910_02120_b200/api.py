@@ -32,7 +32,7 @@ EXPORTS = [
     "ist_set_subnet_range", "ist_packed_layer", "ist_workspace_bytes2", "ist_create2",
     "ist_selftest_wait_expiry", "ist_subnet_slice_shape", "ist_static_partition_status", "ist_local_steps_dx",
     "ist_layer_norm_forward", "ist_layer_norm_workspace_bytes", "ist_layer_norm_backward", "ist_adamw_workspace_bytes",
-    "ist_adamw_step", "ist_adamw_state_values",
+    "ist_adamw_step", "ist_adamw_state_values", "ist_layer_norm_status", "ist_selftest_layer_norm_wait",
 ]
 IST_PART_BALANCED, IST_PART_IID = 0, 1
 IST_STATIC_MAX_NEURONS, IST_STATIC_MAX_SUBNETS = 65536, 64
@@ -155,6 +155,10 @@ def _load() -> ctypes.CDLL:
     lib.ist_layer_norm_workspace_bytes.restype = sz
     lib.ist_layer_norm_backward.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, i32, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
     lib.ist_layer_norm_backward.restype = ctypes.c_int32
+    lib.ist_layer_norm_status.argtypes = [vp]
+    lib.ist_layer_norm_status.restype = ctypes.c_int32
+    lib.ist_selftest_layer_norm_wait.argtypes = [vp, vp, vp, i64, i64, vp, i64, vp]
+    lib.ist_selftest_layer_norm_wait.restype = ctypes.c_int32
     lib.ist_adamw_workspace_bytes.argtypes = [i64]
     lib.ist_adamw_workspace_bytes.restype = sz
     lib.ist_adamw_step.argtypes = [vp, i64, ctypes.POINTER(AdamWArgs), vp, sz, vp]
@@ -579,6 +583,13 @@ def ist_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[
     if given:
         _written([dx])
     return dx, dweight, dbias
+
+
+def ist_layer_norm_status(stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Waits for `stream` (default: the current one) and raises an IstError (IST_ERR_DEVICE_TIMEOUT) if a wait of layer norm's
+    kernels on its device gave up since this was last called; the rows concerned hold NaN."""
+    with torch.cuda.stream(stream):
+        _call(_current_device(), lib.ist_layer_norm_status)
 
 
 def _cuda_device(t: torch.Tensor, name: str) -> torch.device:

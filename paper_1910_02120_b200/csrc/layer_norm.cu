@@ -291,7 +291,7 @@ extern "C" ist_status ist_layer_norm_forward(const void* x_dev, int x_type, int6
   cudaError_t e = cudaSuccess;
   const unsigned blocks = (unsigned)std::min<int64_t>(rows, (int64_t)sm_count() * 8);
   const NormForward rows_args{x_dev, y_dev, x_stride, y_stride, rows / groups, groups, (int)cols, weight_dev, bias_dev,
-                              mean_out_dev, rstd_out_dev, eps};
+                              mean_out_dev, rstd_out_dev, eps, kWaitLimitCycles};
   if (cols > kNormWidest || !norm_forward_rows(rows_args, x_type == IST_T_BF16, y_type == IST_T_BF16, stream, &e)) with_types(x_type, y_type, [&](auto xt, auto yt) {
     using XT = decltype(xt);
     using YT = decltype(yt);
@@ -362,7 +362,7 @@ extern "C" ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, i
   const bool join = sums && parts > 1;
   const NormBackward rows_args{dy_dev, x_dev, dx_out_dev, dy_stride, x_stride, dx_stride, site_rows, groups, (int)cols, weight_dev,
                                mean_dev, rstd_dev, join ? part_sums : dweight_out_dev, join ? part_sums + cols : dbias_out_dev,
-                               join ? 2 * cols : cols, parts};
+                               join ? 2 * cols : cols, parts, kWaitLimitCycles};
   bool taken = cols <= kNormWidest && norm_backward_rows(rows_args, x_type == IST_T_BF16, dy_type == IST_T_BF16, stream, &e);
   if (taken && (e != cudaSuccess || !join)) {
     if (e != cudaSuccess) return fail_call(IST_ERR_CUDA, "ist_layer_norm_backward: %s", cudaGetErrorString(e));
@@ -391,5 +391,36 @@ extern "C" ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, i
                                                                        : launch_join(norm_join_kernel<32>, 32);
   }
   if (e != cudaSuccess) return fail_call(IST_ERR_CUDA, "ist_layer_norm_backward: %s", cudaGetErrorString(e));
+  return IST_OK;
+}
+
+extern "C" ist_status ist_layer_norm_status(void* cuda_stream) {
+  bool forward = false, backward = false;
+  cudaError_t e = norm_forward_gave_up((cudaStream_t)cuda_stream, &forward);
+  if (e == cudaSuccess) e = norm_backward_gave_up((cudaStream_t)cuda_stream, &backward);
+  if (e != cudaSuccess) return fail_call(IST_ERR_CUDA, "ist_layer_norm_status: %s", cudaGetErrorString(e));
+  if (forward || backward) return fail_call(IST_ERR_DEVICE_TIMEOUT, "ist_layer_norm_status: a wait of blocks that share a row gave up");
+  return IST_OK;
+}
+
+extern "C" ist_status ist_selftest_layer_norm_wait(const float* x_dev, const float* dy_dev, const float* stats_dev, int64_t rows,
+                                                   int64_t cols, float* out_dev, int64_t limit_cycles, void* cuda_stream) {
+  const char* why = nullptr;
+  if (rows < 1 || rows > 1 << 16) why = "rows must be in 1..65536";
+  else if (cols <= 16384 || cols > kNormWidest) why = "cols must be in 16385..65536: rows that several blocks share";
+  else if (!x_dev || !out_dev || (dy_dev && !stats_dev)) why = "null rows or statistics";
+  else if (!aligned(x_dev, 4) || !aligned(dy_dev, 4) || !aligned(stats_dev, 4) || !aligned(out_dev, 4)) why = "not aligned to 4 bytes";
+  else if (limit_cycles < 1 || limit_cycles > kWaitLimitCycles) why = "limit_cycles must be in 1..2e9";
+  if (why) return fail_call(IST_ERR_ARG, "ist_selftest_layer_norm_wait: %s", why);
+  cudaError_t e = cudaSuccess;
+  if (!dy_dev) {
+    const NormForward a{x_dev, out_dev, cols, cols, rows, 1, (int)cols, nullptr, nullptr, nullptr, nullptr, 1e-5f, -limit_cycles};
+    norm_forward_rows(a, false, false, (cudaStream_t)cuda_stream, &e);
+  } else {
+    const NormBackward a{dy_dev, x_dev, out_dev, cols, cols, cols, rows, 1, (int)cols, nullptr, stats_dev, stats_dev + rows, nullptr,
+                         nullptr, cols, 1, -limit_cycles};
+    norm_backward_rows(a, false, false, (cudaStream_t)cuda_stream, &e);
+  }
+  if (e != cudaSuccess) return fail_call(IST_ERR_CUDA, "ist_selftest_layer_norm_wait: %s", cudaGetErrorString(e));
   return IST_OK;
 }

@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(NV * V == 16 ? 512 : kNormThreads) norm_backwa
     }
   };
 
-  Turn turn = begin_sums<CL>(sh);
+  Turn turn = begin_sums<CL>(sh, a.wait_limit);
   pdl_wait();
   pdl_trigger();
 #pragma unroll
@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(NV * V == 16 ? 512 : kNormThreads) norm_backwa
     }
     if (V == 1) row_barrier<TPR>();                         // the next fetch writes what the older tile was read from
     if (k < tiles) {
-      if (a.dx) end_row_sums<TPR, CL, 2 * RB>(n, sh, &turn);
+      if (a.dx) end_row_sums<TPR, CL, 2 * RB>(n, sh, &turn, a.wait_limit);
 #pragma unroll
       for (int j = 0; j < RB; ++j) {
         s[j] = n[j];
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(NV * V == 16 ? 512 : kNormThreads) norm_backwa
     }
   }
   copy_wait<0>();
-  if (CL > 1) cluster_sync_all();                           // no block ends while another may write to its sums
+  finish_sums<CL>(turn);
   if (!a.wsum && !a.bsum) return;
   const int64_t at = ((int64_t)part * a.sites + site) * a.sum_ld + c0;
   // the slots' sums are joined in shared memory, slot after slot
@@ -305,5 +305,7 @@ bool norm_backward_rows(const NormBackward& a, bool x_bf16, bool dy_bf16, cudaSt
   return x_bf16 ? dy_bf16 ? dispatch<bf16, bf16>(a, stream, e) : dispatch<bf16, float>(a, stream, e)
                 : dy_bf16 ? dispatch<float, bf16>(a, stream, e) : dispatch<float, float>(a, stream, e);
 }
+
+cudaError_t norm_backward_gave_up(cudaStream_t stream, bool* gave_up) { return read_gave_up(stream, gave_up); }
 
 }  // namespace ist

@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
   };
   auto here = [&](int i) { return (i + 1) * TPR * V <= LEAST || (t + i * TPR) * V < cols; };
 
-  Turn turn = begin_sums<CL>(sh);
+  Turn turn = begin_sums<CL>(sh, a.wait_limit);
   pdl_wait();
   pdl_trigger();
 #pragma unroll
@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
       }
       s[j] = first_of(sum) + second_of(sum);
     }
-    row_sums<TPR, CL, RB>(s, sh, &turn);
+    row_sums<TPR, CL, RB>(s, sh, &turn, a.wait_limit);
     float q[2 * RB];
 #pragma unroll
     for (int j = 0; j < RB; ++j) {
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
       q[j] = first_of(d1) + second_of(d1);
       q[RB + j] = first_of(d2) + second_of(d2);
     }
-    row_sums<TPR, CL, 2 * RB>(q, sh, &turn);
+    row_sums<TPR, CL, 2 * RB>(q, sh, &turn, a.wait_limit);
     pair rstd[RB], shift[RB];
 #pragma unroll
     for (int j = 0; j < RB; ++j) {
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
     if (V == 1) row_barrier<TPR>();                         // the next fetch writes what this tile was read from
   }
   copy_wait<0>();
-  if (CL > 1) cluster_sync_all();                           // no block ends while another may write to its sums
+  finish_sums<CL>(turn);
 }
 
 template <typename XT, typename YT, int V, int NV, int TPR, int RB, int D, int CL, int LEAST>
@@ -296,5 +296,7 @@ bool norm_forward_rows(const NormForward& a, bool x_bf16, bool y_bf16, cudaStrea
   return x_bf16 ? y_bf16 ? dispatch<bf16, bf16>(a, stream, e) : dispatch<bf16, float>(a, stream, e)
                 : y_bf16 ? dispatch<float, bf16>(a, stream, e) : dispatch<float, float>(a, stream, e);
 }
+
+cudaError_t norm_forward_gave_up(cudaStream_t stream, bool* gave_up) { return read_gave_up(stream, gave_up); }
 
 }  // namespace ist

@@ -30,6 +30,7 @@ struct NormForward {
   float* mean;
   float* rstd;
   float eps;
+  long long wait_limit;      // see Turn
 };
 struct NormBackward {
   const void* dy;
@@ -46,11 +47,15 @@ struct NormBackward {
   float* bsum;
   int64_t sum_ld;
   int parts;
+  long long wait_limit;
 };
 
 // norm_forward.cu, norm_backward.cu: false if no kernel takes rows of this width (nothing is launched).
 bool norm_forward_rows(const NormForward& a, bool x_bf16, bool y_bf16, cudaStream_t stream, cudaError_t* e);
 bool norm_backward_rows(const NormBackward& a, bool x_bf16, bool dy_bf16, cudaStream_t stream, cudaError_t* e);
+// Whether a wait of theirs on the current device gave up since the last call; waits for the stream.
+cudaError_t norm_forward_gave_up(cudaStream_t stream, bool* gave_up);
+cudaError_t norm_backward_gave_up(cudaStream_t stream, bool* gave_up);
 // norm_narrow.cu: rows of up to kNormNarrow elements.
 cudaError_t norm_forward_narrow(const NormForward& a, bool x_bf16, bool y_bf16, cudaStream_t stream);
 cudaError_t norm_backward_narrow(const NormBackward& a, bool x_bf16, bool dy_bf16, cudaStream_t stream);
@@ -191,33 +196,53 @@ constexpr int log2_of(int n) { return n <= 1 ? 0 : 1 + log2_of(n / 2); }
 // to its partner, so that N values take N - 1 shuffles and one more for each step left, not one per value and step.
 // RowSums: 2 buffers, used in turn, of [rows of the block][N][warps of a row in the cluster], N up to MOST.  A thread that
 // writes a buffer again has read the sums of the use in between, to which every thread of the row contributed after reading
-// this one, so one barrier per use is enough.  A wait for other blocks' sums that does not end makes them NaN.
+// this one, so one barrier per use is enough.
+//
+// A wait for other blocks' sums that does not end within wait_limit cycles makes them NaN and sets g_gave_up.  The block then
+// neither announces nor sends sums any more (a barrier whose phase has not ended takes no second arrival, and counts only so many
+// bytes), so the cluster's other threads give up in their turn; each waits out the limit once.  A negative limit is the self-test's:
+// all blocks are silent from the start.
 template <int THREADS, int CL, int MOST>
 struct RowSums {
   float part[2 * (THREADS / 32) * CL * MOST];
   uint64_t bar[CL > 1 ? 2 : 1];
+  volatile int silent;       // read ahead of the shuffles it is free; in a register it cost up to 13 % (1000 fp32 rows of 65536)
 };
 struct Turn {
   int buffer, parity;
   bool gave_up;
 };
+__device__ int g_gave_up;    // of this file's kernels
 template <int CL, typename S>
-__device__ __forceinline__ Turn begin_sums(S& sh) {
+__device__ __forceinline__ Turn begin_sums(S& sh, long long wait_limit) {
   if (CL > 1) {
     if (threadIdx.x == 0) {
       mbar_init(&sh.bar[0], 1);
       mbar_init(&sh.bar[CL > 1 ? 1 : 0], 1);
+      sh.silent = wait_limit < 0;
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     cluster_sync_all();
   }
   return Turn{0, 0, false};
 }
+// No block ends while another may write to its sums.  Where all waits ended, all sums that were sent have arrived; after one that
+// gave up, others' may still be on their way when the last of the cluster gets here, and are given time.
+template <int CL>
+__device__ __forceinline__ void finish_sums(const Turn& turn) {
+  if (CL == 1) return;
+  cluster_sync_all();
+  if (turn.gave_up) {
+    const long long begin = clock64();
+    while (clock64() - begin < 200000) {}
+  }
+}
 // The sums' first half: everything up to where other warps' values are needed.
 template <int TPR, int CL, int N, typename S>
 __device__ __forceinline__ void begin_row_sums(float* v, S& sh, const Turn& turn) {
   constexpr int L = TPR < 32 ? TPR : 32;                   // lanes of a row within a warp
   const int lane = threadIdx.x & 31;
+  const int silent = CL > 1 ? sh.silent : 0;
   int n = N, o = L / 2, mine = 0;                          // mine: the value this lane ends with
 #pragma unroll
   for (int s = 0; s < log2_of(N < L ? N : L); ++s, o /= 2) {
@@ -253,15 +278,15 @@ __device__ __forceinline__ void begin_row_sums(float* v, S& sh, const Turn& turn
     if (lane % kShare == 0) b[mine * W + warp] = v[0];
   } else {
     uint64_t* const bar = &sh.bar[turn.buffer];
-    if (threadIdx.x == 0) mbar_expect_tx(bar, W * N * sizeof(float));
-    if (lane % kShare == 0)
+    if (threadIdx.x == 0 && !silent) mbar_expect_tx(bar, W * N * sizeof(float));
+    if (lane % kShare == 0 && !silent)
 #pragma unroll
       for (int q = 0; q < CL; ++q) send_cluster(b + mine * W + cluster_ctarank() * (TPR / 32) + warp, bar, q, v[0]);
   }
 }
 // Their second half: waits for the other warps and adds.
 template <int TPR, int CL, int N, typename S>
-__device__ __forceinline__ void end_row_sums(float* v, S& sh, Turn* turn) {
+__device__ __forceinline__ void end_row_sums(float* v, S& sh, Turn* turn, long long wait_limit) {
   if (TPR <= 32) return;
   constexpr int W = TPR / 32 * CL;
   const int row = threadIdx.x / TPR, lane = threadIdx.x & 31;
@@ -273,8 +298,10 @@ __device__ __forceinline__ void end_row_sums(float* v, S& sh, Turn* turn) {
     if (!turn->gave_up && !mbar_try_wait<true>(bar, turn->parity)) {
       const long long begin = clock64();
       while (!mbar_try_wait<true>(bar, turn->parity))
-        if (clock64() - begin > kWaitLimitCycles) {
+        if (clock64() - begin > (wait_limit < 0 ? -wait_limit : wait_limit)) {
           turn->gave_up = true;
+          sh.silent = 1;
+          *(volatile int*)&g_gave_up = 1;
           break;
         }
     }
@@ -306,9 +333,22 @@ __device__ __forceinline__ void end_row_sums(float* v, S& sh, Turn* turn) {
     for (int i = 0; i < N; ++i) v[i] = __uint_as_float(0x7fc00000u);
 }
 template <int TPR, int CL, int N, typename S>
-__device__ __forceinline__ void row_sums(float* v, S& sh, Turn* turn) {
+__device__ __forceinline__ void row_sums(float* v, S& sh, Turn* turn, long long wait_limit) {
   begin_row_sums<TPR, CL, N>(v, sh, *turn);
-  end_row_sums<TPR, CL, N>(v, sh, turn);
+  end_row_sums<TPR, CL, N>(v, sh, turn, wait_limit);
+}
+
+inline cudaError_t read_gave_up(cudaStream_t stream, bool* gave_up) {
+  int flag = 0;
+  const int none = 0;
+  cudaError_t e = cudaMemcpyFromSymbolAsync(&flag, g_gave_up, sizeof flag, 0, cudaMemcpyDeviceToHost, stream);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+  if (e == cudaSuccess && flag) {
+    e = cudaMemcpyToSymbolAsync(g_gave_up, &none, sizeof none, 0, cudaMemcpyHostToDevice, stream);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+  }
+  *gave_up = flag != 0;
+  return e;
 }
 
 // A launch that may start early (see launch_pdl), of clusters of `cluster` blocks.

@@ -30,3 +30,16 @@ def test_forward_mode_is_refused(api, which, grad):
             trunk.layer_norm(*args)
         with forward_ad._set_fwd_grad_enabled(False):
             trunk.layer_norm(*(t.detach() for t in args))
+
+
+@pytest.mark.parametrize("bad, word", [
+    (dict(rows=0), "rows"), (dict(rows=65537), "rows"), (dict(cols=16384), "cols"), (dict(cols=65537), "cols"), (dict(x=None), "null"),
+    (dict(out=None), "null"), (dict(dy=1 << 21), "statistics"), (dict(x=(1 << 20) + 2), "aligned"), (dict(limit=0), "limit_cycles"),
+    (dict(limit=2_000_000_001), "limit_cycles"), (dict(limit=-5), "limit_cycles"),
+])
+def test_the_self_test_of_waits_refuses(api, bad, word):
+    """Refused before anything is enqueued."""
+    a = {**dict(x=1 << 20, dy=None, stats=None, rows=4, cols=20000, out=1 << 22, limit=1000), **bad}
+    status = api.lib.ist_selftest_layer_norm_wait(a["x"], a["dy"], a["stats"], a["rows"], a["cols"], a["out"], a["limit"], None)
+    assert status == api.IST_ERR_ARG
+    assert word in api.lib.ist_last_error(None).decode()
