@@ -289,15 +289,19 @@ extern "C" ist_status ist_layer_norm_forward(const void* x_dev, int x_type, int6
   if (rows == 0) return IST_OK;
   cudaStream_t stream = (cudaStream_t)cuda_stream;
   cudaError_t e = cudaSuccess;
-  const unsigned blocks = (unsigned)std::min<int64_t>(rows, (int64_t)sm_count() * 8);
-  const NormForward rows_args{x_dev, y_dev, x_stride, y_stride, rows / groups, groups, (int)cols, weight_dev, bias_dev,
-                              mean_out_dev, rstd_out_dev, eps, kWaitLimitCycles};
-  if (cols > kNormWidest || !norm_forward_rows(rows_args, x_type == IST_T_BF16, y_type == IST_T_BF16, stream, &e)) with_types(x_type, y_type, [&](auto xt, auto yt) {
-    using XT = decltype(xt);
-    using YT = decltype(yt);
-    e = launch_pdl(norm_forward_any_kernel<XT, YT>, dim3(blocks), dim3(kThreads), 0, stream, (const XT*)x_dev, x_stride,
-                   rows, cols, rows / groups, weight_dev, bias_dev, eps, (YT*)y_dev, y_stride, mean_out_dev, rstd_out_dev);
-  });
+  if (cols <= kNormWidest) {
+    const NormForward rows_args{x_dev, y_dev, x_stride, y_stride, rows / groups, groups, (int)cols, weight_dev, bias_dev,
+                                mean_out_dev, rstd_out_dev, eps, kWaitLimitCycles};
+    e = norm_forward_rows(rows_args, x_type == IST_T_BF16, y_type == IST_T_BF16, stream);
+  } else {
+    const unsigned blocks = (unsigned)std::min<int64_t>(rows, (int64_t)sm_count() * 8);
+    with_types(x_type, y_type, [&](auto xt, auto yt) {
+      using XT = decltype(xt);
+      using YT = decltype(yt);
+      e = launch_pdl(norm_forward_any_kernel<XT, YT>, dim3(blocks), dim3(kThreads), 0, stream, (const XT*)x_dev, x_stride,
+                     rows, cols, rows / groups, weight_dev, bias_dev, eps, (YT*)y_dev, y_stride, mean_out_dev, rstd_out_dev);
+    });
+  }
   if (e != cudaSuccess) return fail_call(IST_ERR_CUDA, "ist_layer_norm_forward: %s", cudaGetErrorString(e));
   return IST_OK;
 }
@@ -359,28 +363,27 @@ extern "C" ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, i
   if (chunks * groups * std::max(parts, 2) >= (int64_t)1 << 31)
     return fail_call(IST_ERR_UNSUPPORTED, "ist_layer_norm_backward: groups * cols is too large");
   float* const part_sums = (float*)workspace_dev;
-  const bool join = sums && parts > 1;
-  const NormBackward rows_args{dy_dev, x_dev, dx_out_dev, dy_stride, x_stride, dx_stride, site_rows, groups, (int)cols, weight_dev,
-                               mean_dev, rstd_dev, join ? part_sums : dweight_out_dev, join ? part_sums + cols : dbias_out_dev,
-                               join ? 2 * cols : cols, parts, kWaitLimitCycles};
-  bool taken = cols <= kNormWidest && norm_backward_rows(rows_args, x_type == IST_T_BF16, dy_type == IST_T_BF16, stream, &e);
-  if (taken && (e != cudaSuccess || !join)) {
-    if (e != cudaSuccess) return fail_call(IST_ERR_CUDA, "ist_layer_norm_backward: %s", cudaGetErrorString(e));
-    return IST_OK;
+  const bool join = sums && (parts > 1 || cols > kNormWidest);
+  if (cols <= kNormWidest) {
+    const NormBackward rows_args{dy_dev, x_dev, dx_out_dev, dy_stride, x_stride, dx_stride, site_rows, groups, (int)cols, weight_dev,
+                                 mean_dev, rstd_dev, join ? part_sums : dweight_out_dev, join ? part_sums + cols : dbias_out_dev,
+                                 join ? 2 * cols : cols, parts, kWaitLimitCycles};
+    e = norm_backward_rows(rows_args, x_type == IST_T_BF16, dy_type == IST_T_BF16, stream);
+  } else {
+    with_types(x_type, dy_type, [&](auto xt, auto dt) {
+      using XT = decltype(xt);
+      using DT = decltype(dt);
+      if (dx_out_dev)
+        e = launch_pdl(norm_backward_any_kernel<XT, DT>, dim3((unsigned)std::min<int64_t>(rows, (int64_t)sm_count() * 8)),
+                       dim3(kThreads), 0, stream, (const DT*)dy_dev, dy_stride, (const XT*)x_dev, x_stride, rows, cols, site_rows,
+                       weight_dev, mean_dev, rstd_dev, (XT*)dx_out_dev, dx_stride);
+      if (e == cudaSuccess && sums)
+        e = launch_pdl(norm_columns_any_kernel<XT, DT>, dim3((unsigned)(chunks * groups * parts)), dim3(kColumns, kLanes), 0, stream,
+                       (const DT*)dy_dev, dy_stride, (const XT*)x_dev, x_stride, cols, site_rows, groups, parts, mean_dev,
+                       rstd_dev, part_sums);
+    });
   }
-  if (!taken) with_types(x_type, dy_type, [&](auto xt, auto dt) {
-    using XT = decltype(xt);
-    using DT = decltype(dt);
-    if (dx_out_dev)
-      e = launch_pdl(norm_backward_any_kernel<XT, DT>, dim3((unsigned)std::min<int64_t>(rows, (int64_t)sm_count() * 8)),
-                     dim3(kThreads), 0, stream, (const DT*)dy_dev, dy_stride, (const XT*)x_dev, x_stride, rows, cols, site_rows,
-                     weight_dev, mean_dev, rstd_dev, (XT*)dx_out_dev, dx_stride);
-    if (e == cudaSuccess && sums)
-      e = launch_pdl(norm_columns_any_kernel<XT, DT>, dim3((unsigned)(chunks * groups * parts)), dim3(kColumns, kLanes), 0, stream,
-                     (const DT*)dy_dev, dy_stride, (const XT*)x_dev, x_stride, cols, site_rows, groups, parts, mean_dev,
-                     rstd_dev, part_sums);
-  });
-  if (e == cudaSuccess && sums) {
+  if (e == cudaSuccess && join) {
     // as many lanes as keep a thread at about eight parts
     auto blocks = [&](int lanes) { return dim3((unsigned)(ceil_div(cols, kThreads / lanes * 4) * groups * 2)); };
     auto launch_join = [&](auto kernel, int lanes) {
@@ -415,11 +418,11 @@ extern "C" ist_status ist_selftest_layer_norm_wait(const float* x_dev, const flo
   cudaError_t e = cudaSuccess;
   if (!dy_dev) {
     const NormForward a{x_dev, out_dev, cols, cols, rows, 1, (int)cols, nullptr, nullptr, nullptr, nullptr, 1e-5f, -limit_cycles};
-    norm_forward_rows(a, false, false, (cudaStream_t)cuda_stream, &e);
+    e = norm_forward_rows(a, false, false, (cudaStream_t)cuda_stream);
   } else {
     const NormBackward a{dy_dev, x_dev, out_dev, cols, cols, cols, rows, 1, (int)cols, nullptr, stats_dev, stats_dev + rows, nullptr,
                          nullptr, cols, 1, -limit_cycles};
-    norm_backward_rows(a, false, false, (cudaStream_t)cuda_stream, &e);
+    e = norm_backward_rows(a, false, false, (cudaStream_t)cuda_stream);
   }
   if (e != cudaSuccess) return fail_call(IST_ERR_CUDA, "ist_selftest_layer_norm_wait: %s", cudaGetErrorString(e));
   return IST_OK;

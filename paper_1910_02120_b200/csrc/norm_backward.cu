@@ -251,17 +251,18 @@ cudaError_t launch(const NormBackward& a, cudaStream_t stream) {
 }
 
 template <typename XT, typename DT>
-bool dispatch(const NormBackward& a, cudaStream_t stream, cudaError_t* e) {
+cudaError_t dispatch(const NormBackward& a, cudaStream_t stream) {
   constexpr int V = sizeof(XT) == 2 && sizeof(DT) == 2 ? 8 : 4;
   auto fits = [&](const void* p, int64_t ld, int size) { return (((uintptr_t)p | (uintptr_t)(ld * size)) & (V * size - 1)) == 0; };
   const bool pieces = a.cols % V == 0 && fits(a.x, a.x_ld, sizeof(XT)) && fits(a.dy, a.dy_ld, sizeof(DT)) &&
                       (!a.dx || fits(a.dx, a.dx_ld, sizeof(XT)));
   const int n = a.cols;
-  // least: columns that are too many for the line before; of a cluster's block, which may have as little as none, 0
-#define TAKE(least, v, nv, tpr, rb, d, cl)                                                                  \
-  if ((v) > 1 && n == (v) * (nv) * (tpr) * (cl))                                                           \
-    return *e = launch<XT, DT, v, nv, tpr, rb, d, cl, (v) * (nv) * (tpr)>(a, stream), true;               \
-  if (n <= (v) * (nv) * (tpr) * (cl)) return *e = launch<XT, DT, v, nv, tpr, rb, d, cl, least>(a, stream), true
+  // least: columns that are too many for the line before; 0 for a cluster's block, whose part of a row is little more than half of its
+  // class at the least
+#define TAKE(least, v, nv, tpr, rb, d, cl)                                                                             \
+  if constexpr ((v) > 1)                                                                                               \
+    if (n == (v) * (nv) * (tpr) * (cl)) return launch<XT, DT, v, nv, tpr, rb, d, cl, (v) * (nv) * (tpr)>(a, stream);   \
+  if (n <= (v) * (nv) * (tpr) * (cl)) return launch<XT, DT, v, nv, tpr, rb, d, cl, least>(a, stream)
   // Sixteen columns a thread from 257 on, on 512 threads an SM: one block of 512 leaves half the parts' sums that two of 256 leave
   // (rows of 4096, bf16: 47.6 us and 40.6 us).  Two rows at a time where a stage of both types is small (36.9 us against 41 us for
   // bf16 rows of 1024), four rows up to 256 columns.
@@ -295,17 +296,16 @@ bool dispatch(const NormBackward& a, cudaStream_t stream, cudaError_t* e) {
     TAKE(0, 1, 16, 512, R, D, 8);
   }
 #undef TAKE
-  return false;
+  return cudaErrorInvalidValue;          // more than kNormWidest columns
 }
 
 }  // namespace
 
-bool norm_backward_rows(const NormBackward& a, bool x_bf16, bool dy_bf16, cudaStream_t stream, cudaError_t* e) {
-  if (a.cols <= kNormNarrow) return *e = norm_backward_narrow(a, x_bf16, dy_bf16, stream), true;
-  return x_bf16 ? dy_bf16 ? dispatch<bf16, bf16>(a, stream, e) : dispatch<bf16, float>(a, stream, e)
-                : dy_bf16 ? dispatch<float, bf16>(a, stream, e) : dispatch<float, float>(a, stream, e);
+cudaError_t norm_backward_rows(const NormBackward& a, bool x_bf16, bool dy_bf16, cudaStream_t stream) {
+  if (a.cols <= kNormNarrow) return norm_backward_narrow(a, x_bf16, dy_bf16, stream);
+  return x_bf16 ? dy_bf16 ? dispatch<bf16, bf16>(a, stream) : dispatch<bf16, float>(a, stream)
+                : dy_bf16 ? dispatch<float, bf16>(a, stream) : dispatch<float, float>(a, stream);
 }
-
 cudaError_t norm_backward_gave_up(cudaStream_t stream, bool* gave_up) { return read_gave_up(stream, gave_up); }
 
 }  // namespace ist

@@ -13,7 +13,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
   constexpr int kThreads = TPR > kNormThreads ? TPR : kNormThreads, kSlots = kThreads / TPR, kTile = kSlots * RB;
   constexpr int C = NV * V;
   constexpr bool FULL = LEAST == TPR * C;                  // of a block's columns: no piece is missing
-  constexpr bool kKeep = C * (RB + 2) <= 96;               // weight and bias stay in registers
+  static_assert(C * (RB + 2) <= 96, "weight and bias stay in registers beside the rows");
   extern __shared__ __align__(128) char ring[];
   __shared__ RowSums<kThreads, CL, 2 * RB> sh;
   const int t = threadIdx.x % TPR, slot = threadIdx.x / TPR;
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
 #pragma unroll
   for (int k = 0; k < D - 1; ++k) fetch();
   if (V == 1 && todo > 0) fetch_odd(at);
-  pair w[kKeep ? C / 2 : 1], b[kKeep ? C / 2 : 1];
+  pair w[C / 2], b[C / 2];
   int held = -1;
   auto vector = [&](const float* p, int site, float none, int i, float* out) {
 #pragma unroll
@@ -90,16 +90,16 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
   };
   for (; todo > 0; --todo) {
     fetch();
-    if (kKeep && at.site != held) {
+    if (at.site != held) {
       float f[C];
 #pragma unroll
       for (int i = 0; i < NV; ++i) vector(a.weight, at.site, 1.f, i, f + i * V);
 #pragma unroll
-      for (int e = 0; e < C / 2; ++e) w[kKeep ? e : 0] = make_pair2(f[2 * e], f[2 * e + 1]);
+      for (int e = 0; e < C / 2; ++e) w[e] = make_pair2(f[2 * e], f[2 * e + 1]);
 #pragma unroll
       for (int i = 0; i < NV; ++i) vector(a.bias, at.site, 0.f, i, f + i * V);
 #pragma unroll
-      for (int e = 0; e < C / 2; ++e) b[kKeep ? e : 0] = make_pair2(f[2 * e], f[2 * e + 1]);
+      for (int e = 0; e < C / 2; ++e) b[e] = make_pair2(f[2 * e], f[2 * e + 1]);
       held = at.site;
     }
     copy_wait<D - 1>();
@@ -178,30 +178,12 @@ __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_
       constexpr int kPairs = V == 1 ? 1 : V / 2;
       if (V == 1 && i % 2) continue;
       const int p0 = V == 1 ? i / 2 : i * (V / 2);
-      pair wv[kPairs], bv[kPairs];
-      if (kKeep) {
-#pragma unroll
-        for (int e = 0; e < kPairs; ++e) { wv[e] = w[kKeep ? p0 + e : 0]; bv[e] = b[kKeep ? p0 + e : 0]; }
-      } else {
-        float f[2 * kPairs], g[2 * kPairs];
-        vector(a.weight, now.site, 1.f, i, f);
-        vector(a.bias, now.site, 0.f, i, g);
-        if (V == 1) {
-          vector(a.weight, now.site, 1.f, i + 1, f + 1);
-          vector(a.bias, now.site, 0.f, i + 1, g + 1);
-        }
-#pragma unroll
-        for (int e = 0; e < kPairs; ++e) {
-          wv[e] = make_pair2(f[2 * e], f[2 * e + 1]);
-          bv[e] = make_pair2(g[2 * e], g[2 * e + 1]);
-        }
-      }
 #pragma unroll
       for (int j = 0; j < RB; ++j) {
         float o[2 * kPairs];
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
-          const pair r = fma(fma(v[j][p0 + e], rstd[j], shift[j]), wv[e], bv[e]);
+          const pair r = fma(fma(v[j][p0 + e], rstd[j], shift[j]), w[p0 + e], b[p0 + e]);
           o[2 * e] = first_of(r);
           o[2 * e + 1] = second_of(r);
         }
@@ -241,7 +223,7 @@ cudaError_t launch(const NormForward& a, cudaStream_t stream) {
 }
 
 template <typename XT, typename YT>
-bool dispatch(const NormForward& a, cudaStream_t stream, cudaError_t* e) {
+cudaError_t dispatch(const NormForward& a, cudaStream_t stream) {
   constexpr int V = sizeof(XT) == 2 && sizeof(YT) == 2 ? 8 : 4;
   auto fits = [&](const void* p, int64_t ld, int size) { return (((uintptr_t)p | (uintptr_t)(ld * size)) & (V * size - 1)) == 0; };
   const bool pieces = a.cols % V == 0 && fits(a.x, a.x_ld, sizeof(XT)) && fits(a.y, a.y_ld, sizeof(YT));
@@ -250,11 +232,12 @@ bool dispatch(const NormForward& a, cudaStream_t stream, cudaError_t* e) {
   // thread; rows that start anywhere cost more, and a warp alone takes one of up to 1024 (bf16 rows of 1001: 34.9 us, 44.8 us with 64
   // threads a row and a barrier between them).  A row of 16384 goes to one block with 32 columns a thread (35 us for 134 MB read and 67
   // written): two blocks of 16 columns a thread exchange sums twice a row and took 57 us.
-  // least: columns that are too many for the line before; of a cluster's block, which may have as little as none, 0
-#define TAKE(least, v, nv, tpr, rb, d, cl)                                                                  \
-  if ((v) > 1 && n == (v) * (nv) * (tpr) * (cl))                                                           \
-    return *e = launch<XT, YT, v, nv, tpr, rb, d, cl, (v) * (nv) * (tpr)>(a, stream), true;               \
-  if (n <= (v) * (nv) * (tpr) * (cl)) return *e = launch<XT, YT, v, nv, tpr, rb, d, cl, least>(a, stream), true
+  // least: columns that are too many for the line before; 0 for a cluster's block, whose part of a row is little more than half of its
+  // class at the least
+#define TAKE(least, v, nv, tpr, rb, d, cl)                                                                             \
+  if constexpr ((v) > 1)                                                                                               \
+    if (n == (v) * (nv) * (tpr) * (cl)) return launch<XT, YT, v, nv, tpr, rb, d, cl, (v) * (nv) * (tpr)>(a, stream);   \
+  if (n <= (v) * (nv) * (tpr) * (cl)) return launch<XT, YT, v, nv, tpr, rb, d, cl, least>(a, stream)
   if (pieces) {
     TAKE(0, V, 1, 32 / V, 4, 3, 1);
     TAKE(33, V, 1, 64 / V, 4, 3, 1);
@@ -286,17 +269,16 @@ bool dispatch(const NormForward& a, cudaStream_t stream, cudaError_t* e) {
     TAKE(0, 1, 32, 512, 1, 3, 4);
   }
 #undef TAKE
-  return false;
+  return cudaErrorInvalidValue;          // more than kNormWidest columns
 }
 
 }  // namespace
 
-bool norm_forward_rows(const NormForward& a, bool x_bf16, bool y_bf16, cudaStream_t stream, cudaError_t* e) {
-  if (a.cols <= kNormNarrow) return *e = norm_forward_narrow(a, x_bf16, y_bf16, stream), true;
-  return x_bf16 ? y_bf16 ? dispatch<bf16, bf16>(a, stream, e) : dispatch<bf16, float>(a, stream, e)
-                : y_bf16 ? dispatch<float, bf16>(a, stream, e) : dispatch<float, float>(a, stream, e);
+cudaError_t norm_forward_rows(const NormForward& a, bool x_bf16, bool y_bf16, cudaStream_t stream) {
+  if (a.cols <= kNormNarrow) return norm_forward_narrow(a, x_bf16, y_bf16, stream);
+  return x_bf16 ? y_bf16 ? dispatch<bf16, bf16>(a, stream) : dispatch<bf16, float>(a, stream)
+                : y_bf16 ? dispatch<float, bf16>(a, stream) : dispatch<float, float>(a, stream);
 }
-
 cudaError_t norm_forward_gave_up(cudaStream_t stream, bool* gave_up) { return read_gave_up(stream, gave_up); }
 
 }  // namespace ist

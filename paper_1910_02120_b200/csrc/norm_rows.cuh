@@ -50,9 +50,9 @@ struct NormBackward {
   long long wait_limit;
 };
 
-// norm_forward.cu, norm_backward.cu: false if no kernel takes rows of this width (nothing is launched).
-bool norm_forward_rows(const NormForward& a, bool x_bf16, bool y_bf16, cudaStream_t stream, cudaError_t* e);
-bool norm_backward_rows(const NormBackward& a, bool x_bf16, bool dy_bf16, cudaStream_t stream, cudaError_t* e);
+// norm_forward.cu, norm_backward.cu: rows of up to kNormWidest elements.
+cudaError_t norm_forward_rows(const NormForward& a, bool x_bf16, bool y_bf16, cudaStream_t stream);
+cudaError_t norm_backward_rows(const NormBackward& a, bool x_bf16, bool dy_bf16, cudaStream_t stream);
 // Whether a wait of theirs on the current device gave up since the last call; waits for the stream.
 cudaError_t norm_forward_gave_up(cudaStream_t stream, bool* gave_up);
 cudaError_t norm_backward_gave_up(cudaStream_t stream, bool* gave_up);
