@@ -465,7 +465,7 @@ def _rows(t: torch.Tensor, name: str, cols: int, index: int, rows: int = -1) -> 
     kind = _TYPES.get(t.dtype)
     if kind is None:
         raise TypeError(f"unsupported dtype {t.dtype} of {name}")
-    if t.dim() == 0 or t.shape[-1] != cols or (cols > 1 and t.stride(-1) != 1):
+    if t.dim() == 0 or t.shape[-1] != cols or (cols > 1 and t.stride(-1) != 1 and t.numel()):
         _refuse(f"{name}'s last dimension must be {cols} adjacent elements")
     n = t.numel() // cols
     if rows >= 0 and n != rows:

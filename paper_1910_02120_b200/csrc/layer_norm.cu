@@ -324,7 +324,7 @@ extern "C" ist_status ist_layer_norm_backward(const void* dy_dev, int dy_type, i
   if (!why) why = bad_rows(x_dev, x_type, x_stride, rows, cols);
   if (!why) why = bad_rows(dy_dev, dy_type, dy_stride, rows, cols);
   if (!why && dx_out_dev) why = bad_rows(dx_out_dev, x_type, dx_stride, rows, cols);
-  if (!why && !dx_out_dev && !sums) why = "no output is wanted";
+  if (!why && rows && !dx_out_dev && !sums) why = "no output is wanted";      // no rows: dx may have no address
   if (!why && rows && (!mean_dev || !rstd_dev)) why = "the forward pass's mean and rstd are needed";
   if (!why && (!aligned(weight_dev, 4) || !aligned(mean_dev, 4) || !aligned(rstd_dev, 4) || !aligned(dweight_out_dev, 4) ||
                !aligned(dbias_out_dev, 4)))

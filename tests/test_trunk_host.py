@@ -43,3 +43,12 @@ def test_the_self_test_of_waits_refuses(api, bad, word):
     status = api.lib.ist_selftest_layer_norm_wait(a["x"], a["dy"], a["stats"], a["rows"], a["cols"], a["out"], a["limit"], None)
     assert status == api.IST_ERR_ARG
     assert word in api.lib.ist_last_error(None).decode()
+
+
+@pytest.mark.parametrize("dx_stride", [0, 8])
+def test_the_way_back_of_no_rows(api, dx_stride):
+    """An empty dx has no address; nothing is enqueued."""
+    back = api.lib.ist_layer_norm_backward
+    assert back(None, 0, 8, None, 0, 8, 0, 8, 2, None, None, None, None, dx_stride, None, None, None, 0, None) == api.IST_OK
+    assert back(1 << 20, 0, 8, 1 << 21, 0, 8, 4, 8, 2, None, 1 << 22, 1 << 23, None, dx_stride, None, None, None, 0, None) == api.IST_ERR_ARG
+    assert "no output" in api.lib.ist_last_error(None).decode()
