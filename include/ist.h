@@ -387,7 +387,8 @@ enum { IST_T_F32 = 0, IST_T_BF16 = 1 };
  * rounded.  Magnitudes up to 1e16 are always fine; rows of larger values may come out as NaN or as the bias.
  * rows = 0 is allowed.  0 < eps < inf.
  * 1 <= cols <= 2^30, 0 <= rows <= 2^31 - 65536, 1 <= groups < 2^31.  Outputs must not overlap inputs or one another
- * (rows of one buffer that interleave without sharing elements are fine).  Elements between the rows are left as they are.
+ * (rows of one buffer that interleave without sharing elements are fine if their strides are the same number of bytes; others
+ * are refused).  Elements between the rows are left as they are.
  * Very wide rows are shared by several blocks, whose waits for one another are bounded (about a second): a wait that gave up
  * leaves NaN in its row and in those that its block takes after it, and ist_layer_norm_status tells of it.
  */
@@ -454,7 +455,7 @@ ist_status ist_selftest_layer_norm_wait(const float* x_dev, const float* dy_dev,
  * range becomes zero (m) or the smallest code (v: a divisor must not vanish).
  *
  * A tensor with n = 0 or grad = NULL is passed over (its number j still counts).  The tensors' arrays must not overlap one
- * another, but for gradients, which are only read.  Arrays need the alignment of their elements; arrays that start on 16 bytes (on 4
+ * another; gradients, which are only read, may overlap one another, and one may be the very array of its own parameter.  Arrays need the alignment of their elements; arrays that start on 16 bytes (on 4
  * bytes those of 1-byte codes) are faster.  The table of tensors and the arguments are read during the call.
  * step, lr: of this step.  A graph replays the arguments of its capture, so for a captured step they may come from
  * the device instead: step_dev (int64), lr_dev (fp32), not NULL, are read when the kernels run, in place of step and lr.

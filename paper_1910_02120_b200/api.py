@@ -706,6 +706,7 @@ class AdamW:
 
     def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, lr: Optional[float] = None) -> Optional[torch.Tensor]:
         """One step with `grads` (default: the parameters' .grad), all fp32 or all bf16; a None passes its tensor over.
+        They may overlap one another but no parameter, copy or state, except that one may be its own parameter.
         Returns the gradients' norm (fp32 [1]) if they are clipped.  The gradients may be freed or written once the
         work on the stream that follows allows it, as with any asynchronous call."""
         if self.stream is not None and _raw_stream(self.index) != self.stream.cuda_stream:

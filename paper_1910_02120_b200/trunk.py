@@ -37,7 +37,9 @@ class _LayerNorm(torch.autograd.Function):
 def _check_leaves(tensors) -> None:
     """Refuses a capture whose backward pass torch could not capture.  A leaf's accumulation node lives as long as any
     graph that leads to it and stays with the stream it was made on: a backward pass captured while an eager graph of the leaf is
-    alive would synchronise with that stream and break the capture.  So every call notes its stream at the node."""
+    alive would synchronise with that stream and break the capture.  So every call notes its stream at the node.
+    Nodes that only other operations have used carry no note; for these torch's own rule holds, that the leaves of a captured
+    backward pass are not in a live eager graph."""
     stream = torch.cuda.current_stream()
     for t in tensors:
         if t is not None and t.requires_grad and t.grad_fn is None and t.is_cuda:

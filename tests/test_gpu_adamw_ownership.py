@@ -78,3 +78,19 @@ def test_a_captured_step_finds_what_was_moved_before_the_capture(api):
     graph.replay()
     torch.cuda.synchronize()
     assert ((first - 0.9).abs() < 1e-5).all() and ((p.data - 0.8).abs() < 1e-5).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_a_gradient_may_be_its_own_parameter_and_gradients_may_be_one(api, bits, offset):
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    start = torch.randn(3000001 + offset, generator=gen, device=DEV)[offset:]
+    runs = []
+    for own in (True, False):
+        p, q, r = start.clone() if not offset else torch.cat([start[:1], start])[1:], torch.ones(500, device=DEV), torch.ones(500, device=DEV)
+        shared = torch.full((500,), 0.5, device=DEV)
+        opt = api.AdamW([p, q, r], state_bits=bits, max_norm=10.0, seed=1)
+        for _ in range(3):
+            opt.step([p if own else p.clone(), shared, shared if own else shared.clone()])
+        runs.append([p, q, r, *opt.state.values()])
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
