@@ -9,6 +9,7 @@ import ctypes
 import functools
 import operator
 import os
+import weakref
 from array import array
 from typing import List, Optional, Sequence, Tuple
 
@@ -702,7 +703,10 @@ class AdamW:
         self.args.step_dev, self.args.lr_dev = _ptr(self.step_dev), _ptr(self.lr_dev)
         tensors = self._tensors()
         self.written = [t for t in [*params, *(copies or ()), *state.values()] if not t.is_inference()]
-        self.held = list(map(_Tensor.data_ptr, tensors)), list(map(_Tensor.numel, tensors))
+        self.held, self.state_sizes = list(map(_Tensor.data_ptr, tensors)), [t.numel() for t in state.values()]
+        # a storage that goes away leaves its reference here: as long as none has, an address that is the same is the same memory
+        self.freed: list = []
+        self.watched = [weakref.ref(t.untyped_storage(), self.freed.append) for t in tensors]
 
     def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, lr: Optional[float] = None) -> Optional[torch.Tensor]:
         """One step with `grads` (default: the parameters' .grad), all fp32 or all bf16; a None passes its tensor over.
@@ -717,7 +721,7 @@ class AdamW:
         if len(grads) != len(self.sizes):
             _refuse("one gradient (or None) per parameter is needed")
         tensors = self._tensors()
-        if list(map(_Tensor.data_ptr, tensors)) != self.held[0] or list(map(_Tensor.numel, tensors)) != self.held[1]:
+        if self.freed or list(map(_Tensor.data_ptr, tensors)) != self.held or list(map(_Tensor.numel, self.state.values())) != self.state_sizes:
             self._bind()
         index, dtype = self.index, None
         try:                                            # the table's second word of nine is the gradient's address

@@ -56,7 +56,18 @@ def test_a_step_finds_tensors_whose_storage_changed(api, bits):
 
 @pytest.mark.parametrize("bits", [32, 8])
 def test_a_step_refuses_tensors_that_no_longer_fit(api, bits):
-    for change in (lambda o: setattr(o.params[0], "data", o.params[0].data[:200]),                 # the same address
+    buffers = []
+
+    def at_the_same_address(o, name, list_of):
+        """Storage of fewer values where the tensor's lay, as an allocator may give it."""
+        t = list_of(o)[name]
+        buffers.append(np.zeros(4096, np.uint8))
+        t.data = torch.frombuffer(buffers[-1].data, dtype=t.dtype, count=t.numel())
+        o._bind()
+        t.data = torch.frombuffer(buffers[-1].data, dtype=t.dtype, count=t.numel() - 100)
+
+    for change in (lambda o: at_the_same_address(o, 0, lambda o: o.params), lambda o: at_the_same_address(o, 1, lambda o: o.copies),
+                   lambda o: at_the_same_address(o, "exp_avg_sq", lambda o: o.state),
                    lambda o: setattr(o.params[0], "data", o.params[0].data.double()),
                    lambda o: setattr(o.params[0], "data", torch.zeros(600)[::2]),
                    lambda o: setattr(o.copies[1], "data", o.params[1].data), lambda o: o.copies.pop(), lambda o: o.params.pop(),
@@ -97,3 +108,12 @@ def test_eps_has_a_reciprocal_in_fp32(api, eps, fine):
     args = api.AdamWArgs(lr=1e-3, beta1=0.9, beta2=0.999, eps=eps, step=1, state_bits=32)
     assert api.lib.ist_adamw_step(None, 0, args, None, 0, None) == (api.IST_OK if fine else api.IST_ERR_ARG)
     assert fine or "eps" in api.lib.ist_last_error(None).decode()
+
+
+def test_a_view_of_fewer_values_wants_gradients_of_the_old_size(api):
+    params = [torch.ones(300), torch.ones(200)]
+    opt = api.AdamW(params)
+    params[0].data = params[0].data[:200]                     # the same memory, still all there
+    with pytest.raises(api.IstError, match="sizes"):
+        opt.step([torch.ones(200), torch.ones(200)])
+    assert opt.steps == 0 and not api.calls
