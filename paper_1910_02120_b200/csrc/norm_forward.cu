@@ -6,8 +6,8 @@
 namespace ist {
 namespace {
 
-// 51,200 bf16 rows of 1024: 36.7 us, 0.88 of the copy rate; 4096 fp32 rows of 16384 to bf16: 71 us, 0.87.  9600 fp32 rows of 1001,
-// which start anywhere: 14.1 us, against 11.5 us for 1000 columns.
+// 51,200 bf16 rows of 1024: 36.6 us, 0.88 of the copy rate; 4096 fp32 rows of 16384 to bf16: 67 us, 0.92.  9600 fp32 rows of 1001,
+// which start anywhere: 14.1 us, against 11.5 us for 1000 columns; 2^26 bf16 values in rows of 1001 64 us, of 1008 49 us.
 template <typename XT, typename YT, int V, int NV, int TPR, int RB, int D, int CL, int LEAST>
 __global__ void __launch_bounds__(TPR > kNormThreads ? TPR : kNormThreads) norm_forward_kernel(const NormForward a) {
   constexpr int kThreads = TPR > kNormThreads ? TPR : kNormThreads, kSlots = kThreads / TPR, kTile = kSlots * RB;

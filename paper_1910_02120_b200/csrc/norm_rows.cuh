@@ -1,6 +1,6 @@
 // What layer norm's two passes share: rows on their way through shared memory, sums over the threads of a row.
 //
-// TPR threads (8 ... 512) of a block take a row, or its part where a cluster of blocks takes it, each NV pieces of V adjacent
+// TPR threads (4 ... 512) of a block take a row, or its part where a cluster of blocks takes it, each NV pieces of V adjacent
 // elements, piece i of thread t being piece t + i TPR.  Rows come in by asynchronous 16- or 8-byte copies, stages ahead of
 // their use.  Where rows are aligned to pieces (V > 1) a thread copies exactly what it reads itself, so no barrier stands
 // between the two.  Rows that start anywhere (V = 1) are copied in 16-byte pieces too, to the same offset from a 16-byte

@@ -2,6 +2,7 @@
 is set up once per device, not once per process."""
 import os
 import re
+import shutil
 import subprocess
 
 import pytest
@@ -39,6 +40,7 @@ int main() {
 """
 
 
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs a host compiler")
 def test_every_device_has_its_own(tmp_path):
     source, program = tmp_path / "once.cpp", tmp_path / "once"
     source.write_text(PROGRAM)
