@@ -692,7 +692,7 @@ class AdamW:
             if t is not None and (t.device != dev or t.dtype != dtype or t.numel() != 1):
                 _refuse(f"{name} must be one value of {dtype} on {dev}")
         spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
-                       for t in params + (copies or []) + list(state.values()) if t.numel())
+                       for t in [*params, *(copies or ()), *state.values()] if t.numel())
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             _refuse("parameters, copies and states must not overlap")
         self.table["param"] = [p.data_ptr() for p in params]
@@ -708,6 +708,12 @@ class AdamW:
         self.freed: list = []
         self.watched = [weakref.ref(t.untyped_storage(), self.freed.append) for t in tensors]
 
+    def _follow(self) -> None:
+        """Takes over tensors that have moved since the last look."""
+        if (self.freed or list(map(_Tensor.data_ptr, self._tensors())) != self.held
+                or list(map(_Tensor.numel, self.state.values())) != self.state_sizes):
+            self._bind()
+
     def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, lr: Optional[float] = None) -> Optional[torch.Tensor]:
         """One step with `grads` (default: the parameters' .grad), all fp32 or all bf16; a None passes its tensor over.
         They may overlap one another but no parameter, copy or state, except that one may be its own parameter.
@@ -720,9 +726,7 @@ class AdamW:
             grads = [p.grad for p in self.params]
         if len(grads) != len(self.sizes):
             _refuse("one gradient (or None) per parameter is needed")
-        tensors = self._tensors()
-        if self.freed or list(map(_Tensor.data_ptr, tensors)) != self.held or list(map(_Tensor.numel, self.state.values())) != self.state_sizes:
-            self._bind()
+        self._follow()
         index, dtype = self.index, None
         try:                                            # the table's second word of nine is the gradient's address
             self.words[1::9] = array("Q", map(_Tensor.data_ptr, grads))
@@ -768,6 +772,7 @@ class AdamW:
         if self.stream is not None and _raw_stream(self.index) != self.stream.cuda_stream:
             with torch.cuda.stream(self.stream):
                 return self.state_values(dtype)
+        self._follow()
         m, v = self.state["exp_avg"], self.state["exp_avg_sq"]
         if "exp_avg_base" not in self.state:
             return m.to(dtype, copy=True), v.to(dtype, copy=True)

@@ -117,3 +117,14 @@ def test_a_view_of_fewer_values_wants_gradients_of_the_old_size(api):
     with pytest.raises(api.IstError, match="sizes"):
         opt.step([torch.ones(200), torch.ones(200)])
     assert opt.steps == 0 and not api.calls
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_values_of_states_that_no_longer_fit_are_refused(api, bits):
+    """The values are read by the sizes of one state: all have to fit."""
+    for name in ["exp_avg", "exp_avg_sq"] + (["exp_avg_base", "exp_avg_sq_base"] if bits == 8 else []):
+        opt = api.AdamW([torch.ones(300), torch.ones(200)], state_bits=bits)
+        opt.state[name] = opt.state[name][:2]
+        with pytest.raises(api.IstError, match=name):
+            opt.state_values()
+        assert not api.calls
